@@ -48,8 +48,8 @@
  *    (kb & 63) of word kb >> 6 of row r is set iff key block kb belongs to
  *    that row's set.  Several masks "back to back" means mask i starts at
  *    element i * rows * words.
- *  - Alignment: q, k, v, o 16 bytes; workspace 256 bytes; masks, counts
- *    and fp64 arrays 8 bytes; every other pointer 4 bytes.  A misaligned
+ *  - Alignment: q, k, v, o and pools 16 bytes; workspace 256 bytes; masks, the
+ *    counts of wise_mask_overlap and fp64 arrays 8 bytes; every other pointer 4 bytes.  A misaligned
  *    pointer is WISE_ERR_SHAPE.
  */
 #ifndef WISE_H
@@ -380,6 +380,218 @@ size_t wise_select_workspace_bytes(const wise_shape* s);
 /* Upper bound on nnz: batch * heads * nb * (nb + 1) / 2, the number of
  * causally admissible block pairs (-1 for an invalid shape). */
 int64_t wise_support_capacity(const wise_shape* s);
+
+/*
+ * The paged key-value cache
+ * -------------------------
+ * What follows a prompt: single tokens (or a few drafted ones) whose
+ * keys and values are kept.  They live in pages of a pool,
+ *
+ *   pool   : bf16 [planes][pages][kv_heads][page][head_dim].  Plane 2 l holds
+ *            the keys and plane 2 l + 1 the values of layer l by convention;
+ *            the calls that move pages move them in every plane.
+ *   tables : int32 [seqs][max_pages], the page of tokens page*j .. page*j +
+ *            page - 1 of a sequence in column j, -1 in columns past its last.
+ *   lens   : int32 [seqs], tokens of a sequence (0: empty).
+ *   refs   : int32 [pages], how many table entries name the page (free: <= 0).
+ *
+ * all on the device and owned by the caller, who starts with tables -1 and
+ * lens and refs 0.  Sequences share a page by naming it; whoever is to write
+ * into a shared page gets a copy first (wise_cache_reserve).  Ids of
+ * sequences come in device arrays of n <= 1024 entries (n = 0 does nothing),
+ * what each entry got goes to device arrays, and no call waits for the
+ * device: a step of a serving loop (trim, fork, reserve, append, attend)
+ * can be captured in one HIP graph.  Calls that share tables, lens, refs, pool or
+ * a workspace must be ordered, by one stream or by events.  An entry whose
+ * id lies outside 0..seqs-1 does nothing, and so does one whose id an earlier
+ * entry of the same call already names (in wise_cache_append and
+ * wise_prefix_attn an id may repeat, see there).  Page ids
+ * outside 0..pages-1 are never followed.
+ */
+typedef struct {
+  int32_t pages;     /* pages of the pool                                    */
+  int32_t page;      /* tokens of a page: 16, 32, 64 or 128                  */
+  int32_t kv_heads;
+  int32_t head_dim;  /* 64, 96 or 128                                        */
+  int32_t planes;    /* planes of the pool: 2 x layers                       */
+  int32_t seqs;      /* rows of tables and lens                              */
+  int32_t max_pages; /* columns of tables; max_pages * page < 2^31           */
+} wise_cache;
+
+/*
+ * wise_cache_fork — sequence dst[i] becomes a copy of src[i]: it names the
+ * same pages (refs + 1 each) and has the same length.  No keys or values move.
+ *
+ * Every entry reads the state before the call.  It is refused, and leaves
+ * everything as it is, when dst[i] is not empty, when src[i] is also a
+ * destination of the call, or by the rules above (an earlier entry with the
+ * same dst wins; a source may be named any number of times).
+ *
+ *   src, dst : int32 [n], device, read-only.
+ *   done     : int32 [n] or NULL, written: 1, or 0 for a refused entry.
+ * Errors: WISE_ERR_NULL, WISE_ERR_SHAPE (also n < 0), WISE_ERR_UNSUPPORTED
+ *         (also n > 1024), WISE_ERR_HIP.
+ */
+wise_status wise_cache_fork(const wise_cache* c, int32_t n, const int32_t* src,
+                            const int32_t* dst, int32_t* tables, int32_t* lens,
+                            int32_t* refs, int32_t* done, void* hip_stream);
+
+/*
+ * wise_cache_trim — drops the tokens of sequence seq_ids[i] from new_lens[i]
+ * on (drafts that were not accepted, a finished request): its length becomes
+ * min(length, max(new_lens[i], 0)), pages wholly past it lose a reference, their
+ * table entries become -1.
+ *
+ *   seq_ids  : int32 [n], device, read-only.
+ *   new_lens : int32 [n], device, read-only, or NULL: 0 for every entry (the
+ *              sequences are freed).
+ * Errors: as wise_cache_fork.
+ */
+wise_status wise_cache_trim(const wise_cache* c, int32_t n,
+                            const int32_t* seq_ids, const int32_t* new_lens,
+                            int32_t* tables, int32_t* lens, int32_t* refs,
+                            void* hip_stream);
+
+/*
+ * wise_cache_reserve — makes sequence seq_ids[i] counts[i] tokens longer and
+ * gives it the pages that these need, so that wise_cache_append can write
+ * them.  A last page that is partly filled and that other table entries name
+ * too (refs > 1 before the call) is first replaced by a copy of its own: the
+ * tokens it holds, in every plane.
+ *
+ * Pages are handed out in ascending order of id, to the entries in order and to each
+ * in ascending order of its columns.  An entry is refused (granted 0,
+ * nothing changed) by the rules above, when counts[i] <= 0, when the sequence would
+ * outgrow max_pages * page tokens, or when it needs pages and
+ * these and those that the entries before it need (but for entries refused for the
+ * other reasons) are more than were free before the call.  Pages
+ * that lose their last reference here are free from the next call on.
+ *
+ *   seq_ids, counts : int32 [n], device, read-only.
+ *   granted   : int32 [n], written: counts[i], or 0 for a refused entry.
+ *   pool      : all planes.
+ *   workspace : device scratch of wise_cache_workspace_bytes(c) bytes, 256-byte
+ *               aligned; contents on entry are ignored.
+ * Errors: as wise_cache_fork, and WISE_ERR_WORKSPACE.
+ */
+wise_status wise_cache_reserve(const wise_cache* c, int32_t n,
+                               const int32_t* seq_ids, const int32_t* counts,
+                               int32_t* tables, int32_t* lens, int32_t* refs,
+                               int32_t* granted, void* pool, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+
+/*
+ * wise_cache_append — writes the newest counts[i] tokens of sequence
+ * seq_ids[i] (positions lens - counts[i] .. lens - 1, after wise_cache_reserve)
+ * in one layer.  Tokens that fall on positions below 0, or on columns without
+ * a page, are skipped.  Every id should occur once: an id that repeats
+ * has its tokens written by each entry, in no order.
+ *
+ *   tokens  : token rows of k and v per entry, 1 or more.
+ *   seq_ids : int32 [n], counts : int32 [n], device, read-only; counts[i] is
+ *             taken as min(max(counts[i], 0), tokens).  wise_cache_reserve's
+ *             `granted` is what to pass.
+ *   k, v    : bf16 [n][kv_heads][tokens][head_dim], read-only; rows from
+ *             counts[i] on are not read.
+ *   k_pool, v_pool : the layer's two planes, [pages][kv_heads][page][head_dim].
+ * Errors: as wise_cache_fork (WISE_ERR_SHAPE also for tokens < 1 and for
+ *         n * kv_heads * tokens > 2^31 - 1).
+ */
+wise_status wise_cache_append(const wise_cache* c, int32_t n, int32_t tokens,
+                              const int32_t* seq_ids, const int32_t* counts,
+                              const void* k, const void* v,
+                              const int32_t* tables, const int32_t* lens,
+                              void* k_pool, void* v_pool, void* hip_stream);
+
+/*
+ * wise_cache_compact — moves the pages in use to the front of the pool: with
+ * L of them, the k-th one of id >= L (ascending) moves to the k-th free page
+ * of id < L, in every plane, and takes its references along; table entries
+ * follow.  Afterwards pages 0..L-1 are in use and the others free.
+ *
+ *   live      : int32 [1] or NULL, device, written: L.
+ *   workspace : as for wise_cache_reserve.
+ * Errors: as wise_cache_reserve.
+ */
+wise_status wise_cache_compact(const wise_cache* c, int32_t* tables,
+                               int32_t* refs, void* pool, int32_t* live,
+                               void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/*
+ * wise_cache_shared — what neighbours of a batch have in common: shared[b] is
+ * the number of leading pages that sequence b and sequence b - 1 both name and
+ * both fill, or 0 if that is less than min_pages; shared[0] = 0.  The argument of
+ * wise_prefix_attn.
+ *
+ *   batch   : 1 .. 1024 sequences, in the order of the attention call.
+ *   seq_ids : int32 [batch], device, read-only, or NULL: sequence b is table row b.
+ * Errors: as wise_cache_fork (WISE_ERR_SHAPE also for batch > seqs without
+ *         seq_ids).
+ */
+wise_status wise_cache_shared(const wise_cache* c, int32_t batch,
+                              int32_t min_pages, const int32_t* seq_ids,
+                              const int32_t* tables, const int32_t* lens,
+                              int32_t* shared, void* hip_stream);
+
+/* Bytes of device workspace wise_cache_reserve and wise_cache_compact need
+ * (0 for an invalid cache). */
+size_t wise_cache_workspace_bytes(const wise_cache* c);
+
+/* The newest q_len tokens of `batch` sequences.  heads must be a multiple of
+ * the cache's kv_heads (query head h reads key-value head h / (heads /
+ * kv_heads)), heads / kv_heads * q_len <= 128, batch <= 1024.  scale <= 0
+ * selects 1/sqrt(head_dim). */
+typedef struct {
+  int32_t batch;
+  int32_t heads;
+  int32_t q_len;
+  float scale;
+} wise_queries;
+
+/*
+ * wise_prefix_attn — attention of the newest q_len tokens of every sequence
+ * of a batch over its pages (Section 3, eq. "recurrent_attention", with keys
+ * and values of the earlier positions kept): token t of sequence b sits at
+ * position i = lens - q_len + t and attends the positions j <= i.
+ *
+ * Runs of sequences that begin with the same pages have these read once for
+ * all: shared[b] is the number of leading pages that sequence b shares
+ * with sequence b - 1 (wise_cache_shared counts them).  shared[b] <= 0 starts a
+ * run, and what a run reads once is the least shared[b] of its other sequences, at
+ * most the whole pages that all queries of the run see, through the table
+ * of its first sequence.  shared changes which pages are read together, and the
+ * last bits, not what is computed.
+ *
+ *   q         : bf16 [batch][heads][q_len][head_dim], read-only.
+ *   k_pool, v_pool : the layer's two planes, read-only.
+ *   tables, lens : read-only.  A length is taken as at most max_pages * page.
+ *               Positions from a sequence's length on, and positions on a page id outside
+ *               0..pages-1, are not attended, whatever the pool holds there.
+ *   seq_ids   : int32 [batch], device, or NULL: sequence b is table row b.  An
+ *               id may repeat; one outside 0..seqs-1 is an empty sequence.
+ *   shared    : int32 [batch], device, or NULL: nothing is shared.
+ *   o         : bf16 [batch][heads][q_len][head_dim], written.  A row that sees
+ *               no position is zero (and its lse -inf).
+ *   lse       : fp32 [batch][heads][q_len] or NULL: natural log of the sum.
+ *   workspace : device scratch of wise_prefix_workspace_bytes(c, a) bytes, 256-byte
+ *               aligned; contents on entry are ignored.
+ * Bitwise deterministic: the sums of a row run in an order that lens and shared
+ * fix.
+ * Errors: WISE_ERR_NULL, WISE_ERR_SHAPE, WISE_ERR_UNSUPPORTED, WISE_ERR_RANGE
+ *         (scale), WISE_ERR_WORKSPACE, WISE_ERR_HIP.
+ */
+wise_status wise_prefix_attn(const wise_cache* c, const wise_queries* a,
+                             const void* q, const void* k_pool,
+                             const void* v_pool, const int32_t* tables,
+                             const int32_t* lens, const int32_t* seq_ids,
+                             const int32_t* shared, void* o, float* lse,
+                             void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* Bytes of device workspace wise_prefix_attn needs (0 for invalid
+ * arguments). */
+size_t wise_prefix_workspace_bytes(const wise_cache* c, const wise_queries* a);
 
 /* Static, NUL-terminated description of a status code. */
 const char* wise_status_string(wise_status st);

@@ -7,6 +7,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "wise.h"
 #include "wise_kernels.hpp"
 
@@ -48,6 +50,50 @@ wise_status check_qkvo(const void* q, const void* k, const void* v, const void* 
   if (!q || !k || !v || !o) return WISE_ERR_NULL;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16))
     return WISE_ERR_SHAPE;
+  return WISE_OK;
+}
+
+// Geometry of a paged cache; fills the validated one.
+wise_status check_cache(const wise_cache* c, wise::Cache* out) {
+  if (c == nullptr) return WISE_ERR_NULL;
+  if (c->pages <= 0 || c->page <= 0 || c->kv_heads <= 0 || c->head_dim <= 0 || c->planes <= 0 || c->seqs <= 0 ||
+      c->max_pages <= 0)
+    return WISE_ERR_SHAPE;
+  if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WISE_ERR_UNSUPPORTED;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return WISE_ERR_UNSUPPORTED;
+  // Token positions are int32; byte offsets into a pool are 64-bit.
+  if ((int64_t)c->max_pages * c->page > kI32Max || c->pages > wise::kMaxPages) return WISE_ERR_SHAPE;
+  if ((int64_t)c->kv_heads * c->page * c->head_dim > kI32Max) return WISE_ERR_SHAPE;
+  *out = wise::Cache{c->pages, c->page, c->kv_heads, c->head_dim, c->planes, c->seqs, c->max_pages};
+  return WISE_OK;
+}
+
+// The same for a call that names n sequences.
+wise_status check_entries(const wise_cache* c, int32_t n, wise::Cache* out) {
+  const wise_status st = check_cache(c, out);
+  if (st != WISE_OK) return st;
+  if (n < 0) return WISE_ERR_SHAPE;
+  return n > wise::kMaxEntries ? WISE_ERR_UNSUPPORTED : WISE_OK;
+}
+
+wise_status check_queries(const wise_cache* c, const wise_queries* a, wise::Cache* cache, wise::Queries* out) {
+  const wise_status st = check_cache(c, cache);
+  if (st != WISE_OK) return st;
+  if (a == nullptr) return WISE_ERR_NULL;
+  if (a->batch <= 0 || a->heads <= 0 || a->q_len <= 0 || a->heads % c->kv_heads != 0) return WISE_ERR_SHAPE;
+  if (a->batch > wise::kMaxEntries || (int64_t)(a->heads / c->kv_heads) * a->q_len > wise::kMaxQueryRows)
+    return WISE_ERR_UNSUPPORTED;
+  if (isnan(a->scale) || isinf(a->scale)) return WISE_ERR_RANGE;
+  *out = wise::Queries{a->batch, a->heads, a->q_len, a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)};
+  return WISE_OK;
+}
+
+// Non-NULL and 4-byte aligned: the index arrays of a call.
+wise_status check_ints(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (p == nullptr) return WISE_ERR_NULL;
+  for (const void* p : ps)
+    if (!aligned(p, 4)) return WISE_ERR_SHAPE;
   return WISE_OK;
 }
 
@@ -260,6 +306,108 @@ int64_t wise_support_capacity(const wise_shape* s) {
   wise::Dims d;
   if (check_shape(s, &d) != WISE_OK) return -1;
   return (int64_t)d.bh * d.nb * (d.nb + 1) / 2;
+}
+
+wise_status wise_cache_fork(const wise_cache* c, int32_t n, const int32_t* src, const int32_t* dst, int32_t* tables,
+                            int32_t* lens, int32_t* refs, int32_t* done, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, n, &d);
+  if (st != WISE_OK || n == 0) return st;
+  if ((st = check_ints({src, dst, tables, lens, refs})) != WISE_OK) return st;
+  if (done && !aligned(done, 4)) return WISE_ERR_SHAPE;
+  return from_hip(wise::launch_cache_fork(d, n, src, dst, tables, lens, refs, done, (hipStream_t)hip_stream));
+}
+
+wise_status wise_cache_trim(const wise_cache* c, int32_t n, const int32_t* seq_ids, const int32_t* new_lens, int32_t* tables,
+                            int32_t* lens, int32_t* refs, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, n, &d);
+  if (st != WISE_OK || n == 0) return st;
+  if ((st = check_ints({seq_ids, tables, lens, refs})) != WISE_OK) return st;
+  if (new_lens && !aligned(new_lens, 4)) return WISE_ERR_SHAPE;
+  return from_hip(wise::launch_cache_trim(d, n, seq_ids, new_lens, tables, lens, refs, (hipStream_t)hip_stream));
+}
+
+wise_status wise_cache_reserve(const wise_cache* c, int32_t n, const int32_t* seq_ids, const int32_t* counts, int32_t* tables,
+                               int32_t* lens, int32_t* refs, int32_t* granted, void* pool, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, n, &d);
+  if (st != WISE_OK || n == 0) return st;
+  if (!pool || !workspace) return WISE_ERR_NULL;
+  if ((st = check_ints({seq_ids, counts, tables, lens, refs, granted})) != WISE_OK) return st;
+  if (!aligned(pool, 16) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
+  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
+  return from_hip(wise::launch_cache_reserve(d, n, seq_ids, counts, tables, lens, refs, granted, pool, workspace,
+                                             (hipStream_t)hip_stream));
+}
+
+wise_status wise_cache_append(const wise_cache* c, int32_t n, int32_t tokens, const int32_t* seq_ids, const int32_t* counts,
+                              const void* k, const void* v, const int32_t* tables, const int32_t* lens, void* k_pool,
+                              void* v_pool, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, n, &d);
+  if (st != WISE_OK) return st;
+  if (tokens < 1) return WISE_ERR_SHAPE;
+  if (n == 0) return WISE_OK;
+  if ((st = check_ints({seq_ids, counts, tables, lens})) != WISE_OK) return st;
+  if ((st = check_qkvo(k, v, k_pool, v_pool)) != WISE_OK) return st;
+  if ((int64_t)n * d.kv_heads > kI32Max / tokens) return WISE_ERR_SHAPE;
+  return from_hip(wise::launch_cache_append(d, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
+                                            (hipStream_t)hip_stream));
+}
+
+wise_status wise_cache_compact(const wise_cache* c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_cache(c, &d);
+  if (st != WISE_OK) return st;
+  if (!pool || !workspace) return WISE_ERR_NULL;
+  if ((st = check_ints({tables, refs})) != WISE_OK) return st;
+  if (!aligned(pool, 16) || (live && !aligned(live, 4)) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
+  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
+  return from_hip(wise::launch_cache_compact(d, tables, refs, pool, live, workspace, (hipStream_t)hip_stream));
+}
+
+wise_status wise_cache_shared(const wise_cache* c, int32_t batch, int32_t min_pages, const int32_t* seq_ids,
+                              const int32_t* tables, const int32_t* lens, int32_t* shared, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, batch, &d);
+  if (st != WISE_OK) return st;
+  if (batch < 1 || (seq_ids == nullptr && batch > d.seqs)) return WISE_ERR_SHAPE;
+  if ((st = check_ints({tables, lens, shared})) != WISE_OK) return st;
+  if (seq_ids && !aligned(seq_ids, 4)) return WISE_ERR_SHAPE;
+  return from_hip(wise::launch_cache_shared(d, batch, min_pages, seq_ids, tables, lens, shared, (hipStream_t)hip_stream));
+}
+
+size_t wise_cache_workspace_bytes(const wise_cache* c) {
+  wise::Cache d;
+  return check_cache(c, &d) == WISE_OK ? wise::cache_workspace_bytes(d) : 0;
+}
+
+wise_status wise_prefix_attn(const wise_cache* c, const wise_queries* a, const void* q, const void* k_pool, const void* v_pool,
+                             const int32_t* tables, const int32_t* lens, const int32_t* seq_ids, const int32_t* shared, void* o,
+                             float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise::Queries x;
+  wise_status st = check_queries(c, a, &d, &x);
+  if (st != WISE_OK) return st;
+  if (seq_ids == nullptr && x.batch > d.seqs) return WISE_ERR_SHAPE;
+  if ((st = check_qkvo(q, k_pool, v_pool, o)) != WISE_OK) return st;
+  if ((st = check_ints({tables, lens})) != WISE_OK) return st;
+  if (!workspace) return WISE_ERR_NULL;
+  if ((seq_ids && !aligned(seq_ids, 4)) || (shared && !aligned(shared, 4)) || (lse && !aligned(lse, 4)) ||
+      !aligned(workspace, 256))
+    return WISE_ERR_SHAPE;
+  if (workspace_bytes < wise::prefix_workspace_bytes(d, x)) return WISE_ERR_WORKSPACE;
+  return from_hip(wise::launch_prefix(d, x, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace,
+                                      (hipStream_t)hip_stream));
+}
+
+size_t wise_prefix_workspace_bytes(const wise_cache* c, const wise_queries* a) {
+  wise::Cache d;
+  wise::Queries x;
+  return check_queries(c, a, &d, &x) == WISE_OK ? wise::prefix_workspace_bytes(d, x) : 0;
 }
 
 const char* wise_status_string(wise_status st) {

@@ -15,6 +15,19 @@ struct Dims {
   float scale;
 };
 
+// Validated paged cache and the queries that read it (wise_cache, wise_queries).
+struct Cache {
+  int pages, page, kv_heads, head_dim, planes, seqs, max_pages;
+};
+struct Queries {
+  int batch, heads, q_len;
+  float scale;
+};
+
+constexpr int kMaxEntries = 1024;       // sequences named by one call on a cache
+constexpr int kMaxQueryRows = 128;      // query rows of a sequence per key-value head
+constexpr int kMaxPages = 1 << 27;      // of a pool: 256 GB of the smallest pages
+
 constexpr int kMaxSelectBlocks = 1024;  // selection keeps a row's candidates in LDS
 
 hipError_t launch_dense(const Dims& s, const void* q, const void* k, const void* v, void* o,
@@ -52,5 +65,23 @@ hipError_t launch_mask_overlap(const Dims& s, const uint64_t* a, const uint64_t*
 hipError_t launch_support_mass(const Dims& s, const float* r, const int32_t* row_ptr,
                                const int32_t* col_idx, double* row_mass, double* totals,
                                hipStream_t st);
+
+hipError_t launch_cache_fork(const Cache& c, int n, const int32_t* src, const int32_t* dst, int32_t* tables, int32_t* lens,
+                             int32_t* refs, int32_t* done, hipStream_t st);
+hipError_t launch_cache_trim(const Cache& c, int n, const int32_t* ids, const int32_t* new_lens, int32_t* tables, int32_t* lens,
+                             int32_t* refs, hipStream_t st);
+hipError_t launch_cache_reserve(const Cache& c, int n, const int32_t* ids, const int32_t* counts, int32_t* tables, int32_t* lens,
+                                int32_t* refs, int32_t* granted, void* pool, void* ws, hipStream_t st);
+hipError_t launch_cache_append(const Cache& c, int n, int tokens, const int32_t* ids, const int32_t* counts, const void* k,
+                               const void* v, const int32_t* tables, const int32_t* lens, void* kp, void* vp, hipStream_t st);
+hipError_t launch_cache_compact(const Cache& c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,
+                                hipStream_t st);
+hipError_t launch_cache_shared(const Cache& c, int batch, int min_pages, const int32_t* ids, const int32_t* tables,
+                               const int32_t* lens, int32_t* shared, hipStream_t st);
+size_t cache_workspace_bytes(const Cache& c);
+hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const void* kp, const void* vp, const int32_t* tables,
+                         const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse, void* ws,
+                         hipStream_t st);
+size_t prefix_workspace_bytes(const Cache& c, const Queries& a);
 
 }  // namespace wise

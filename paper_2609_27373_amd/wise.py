@@ -33,7 +33,10 @@ EXPORTS = ("wise_dense_attn_accum", "wise_select_support", "wise_select_support_
            "wise_support_mass", "wise_mass_workspace_bytes", "wise_mass_workspace_min_bytes",
            "wise_mask_words",
            "wise_select_workspace_bytes",
-           "wise_support_capacity", "wise_status_string", "wise_abi_version")
+           "wise_support_capacity", "wise_cache_fork", "wise_cache_trim", "wise_cache_reserve",
+           "wise_cache_append", "wise_cache_compact", "wise_cache_shared",
+           "wise_cache_workspace_bytes", "wise_prefix_attn", "wise_prefix_workspace_bytes",
+           "wise_status_string", "wise_abi_version")
 
 
 class WiseError(RuntimeError):
@@ -59,6 +62,25 @@ def make_shape(batch: int, heads: int, seq_len: int, head_dim: int, block: int,
                scale: float = 0.0, kv_heads: int = 0) -> wise_shape:
     """kv_heads = 0: one key-value head per query head."""
     return wise_shape(batch, heads, seq_len, head_dim, block, scale, kv_heads)
+
+
+class wise_cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("pages", "page", "kv_heads", "head_dim", "planes",
+                                              "seqs", "max_pages")]
+
+
+class wise_queries(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("q_len", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+def make_cache(pages: int, page: int, kv_heads: int, head_dim: int, planes: int, seqs: int,
+               max_pages: int) -> wise_cache:
+    return wise_cache(pages, page, kv_heads, head_dim, planes, seqs, max_pages)
+
+
+def make_queries(batch: int, heads: int, q_len: int = 1, scale: float = 0.0) -> wise_queries:
+    return wise_queries(batch, heads, q_len, scale)
 
 
 _LIB: Optional[ctypes.CDLL] = None
@@ -109,6 +131,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.wise_select_workspace_bytes.restype = ctypes.c_size_t
     lib.wise_support_capacity.argtypes = [S]
     lib.wise_support_capacity.restype = ctypes.c_int64
+    C, Q, I, Z = ctypes.POINTER(wise_cache), ctypes.POINTER(wise_queries), ctypes.c_int32, ctypes.c_size_t
+    for fn, args in (("wise_cache_fork", [C, I, P, P, P, P, P, P, P]),
+                     ("wise_cache_trim", [C, I, P, P, P, P, P, P]),
+                     ("wise_cache_reserve", [C, I, P, P, P, P, P, P, P, P, Z, P]),
+                     ("wise_cache_append", [C, I, I, P, P, P, P, P, P, P, P, P]),
+                     ("wise_cache_compact", [C, P, P, P, P, P, Z, P]),
+                     ("wise_cache_shared", [C, I, I, P, P, P, P, P]),
+                     ("wise_prefix_attn", [C, Q, P, P, P, P, P, P, P, P, P, P, Z, P])):
+        getattr(lib, fn).argtypes = args
+        getattr(lib, fn).restype = ctypes.c_int
+    lib.wise_cache_workspace_bytes.argtypes = [C]
+    lib.wise_cache_workspace_bytes.restype = Z
+    lib.wise_prefix_workspace_bytes.argtypes = [C, Q]
+    lib.wise_prefix_workspace_bytes.restype = Z
     lib.wise_status_string.argtypes = [ctypes.c_int]
     lib.wise_status_string.restype = ctypes.c_char_p
     lib.wise_abi_version.argtypes = []
@@ -306,6 +342,109 @@ def wise_select_workspace_bytes(s: wise_shape) -> int:
 
 def wise_support_capacity(s: wise_shape) -> int:
     return int(_lib().wise_support_capacity(ctypes.byref(s)))
+
+
+def _cache_numel(c: wise_cache):
+    """Elements of (one plane of the pool, tables, lens, refs)."""
+    return (c.pages * c.kv_heads * c.page * c.head_dim, c.seqs * c.max_pages, c.seqs, c.pages)
+
+
+def _entries(t, n, name):
+    if n is None:
+        n = t.numel()
+    return n, _ptr(t, torch.int32, name, n)
+
+
+def wise_cache_fork(c: wise_cache, src, dst, tables, lens, refs, done=None, stream=None) -> None:
+    _, nt, ns, nr = _cache_numel(c)
+    i32 = torch.int32
+    n, ps = _entries(src, None, "src")
+    _check(_lib().wise_cache_fork(
+        ctypes.byref(c), n, ps, _ptr(dst, i32, "dst", n), _ptr(tables, i32, "tables", nt),
+        _ptr(lens, i32, "lens", ns), _ptr(refs, i32, "refs", nr), _ptr(done, i32, "done", n),
+        _stream(stream)), "wise_cache_fork")
+
+
+def wise_cache_trim(c: wise_cache, seq_ids, new_lens, tables, lens, refs, stream=None) -> None:
+    _, nt, ns, nr = _cache_numel(c)
+    i32 = torch.int32
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    _check(_lib().wise_cache_trim(
+        ctypes.byref(c), n, ps, _ptr(new_lens, i32, "new_lens", n), _ptr(tables, i32, "tables", nt),
+        _ptr(lens, i32, "lens", ns), _ptr(refs, i32, "refs", nr), _stream(stream)),
+        "wise_cache_trim")
+
+
+def wise_cache_reserve(c: wise_cache, seq_ids, counts, tables, lens, refs, granted, pool, workspace,
+                       stream=None) -> None:
+    npl, nt, ns, nr = _cache_numel(c)
+    i32 = torch.int32
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    ws_bytes = workspace.numel() * workspace.element_size()
+    _check(_lib().wise_cache_reserve(
+        ctypes.byref(c), n, ps, _ptr(counts, i32, "counts", n), _ptr(tables, i32, "tables", nt),
+        _ptr(lens, i32, "lens", ns), _ptr(refs, i32, "refs", nr), _ptr(granted, i32, "granted", n),
+        _ptr(pool, torch.bfloat16, "pool", npl * c.planes), _ptr(workspace, None, "workspace"),
+        ctypes.c_size_t(ws_bytes), _stream(stream)), "wise_cache_reserve")
+
+
+def wise_cache_append(c: wise_cache, tokens: int, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
+                      stream=None) -> None:
+    npl, nt, ns, _ = _cache_numel(c)
+    i32, bf = torch.int32, torch.bfloat16
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    rows = n * c.kv_heads * tokens * c.head_dim
+    _check(_lib().wise_cache_append(
+        ctypes.byref(c), n, tokens, ps, _ptr(counts, i32, "counts", n), _ptr(k, bf, "k", rows),
+        _ptr(v, bf, "v", rows), _ptr(tables, i32, "tables", nt), _ptr(lens, i32, "lens", ns),
+        _ptr(k_pool, bf, "k_pool", npl), _ptr(v_pool, bf, "v_pool", npl), _stream(stream)),
+        "wise_cache_append")
+
+
+def wise_cache_compact(c: wise_cache, tables, refs, pool, live=None, workspace=None,
+                       stream=None) -> None:
+    npl, nt, _, nr = _cache_numel(c)
+    i32 = torch.int32
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().wise_cache_compact(
+        ctypes.byref(c), _ptr(tables, i32, "tables", nt), _ptr(refs, i32, "refs", nr),
+        _ptr(pool, torch.bfloat16, "pool", npl * c.planes), _ptr(live, i32, "live", 1),
+        _ptr(workspace, None, "workspace"), ctypes.c_size_t(ws_bytes), _stream(stream)),
+        "wise_cache_compact")
+
+
+def wise_cache_shared(c: wise_cache, batch: int, min_pages: int, seq_ids, tables, lens, shared,
+                      stream=None) -> None:
+    _, nt, ns, _ = _cache_numel(c)
+    i32 = torch.int32
+    _check(_lib().wise_cache_shared(
+        ctypes.byref(c), batch, min_pages, _ptr(seq_ids, i32, "seq_ids", batch),
+        _ptr(tables, i32, "tables", nt), _ptr(lens, i32, "lens", ns),
+        _ptr(shared, i32, "shared", batch), _stream(stream)), "wise_cache_shared")
+
+
+def wise_prefix_attn(c: wise_cache, a: wise_queries, q, k_pool, v_pool, tables, lens, seq_ids, shared,
+                     o, lse=None, workspace=None, stream=None) -> None:
+    npl, nt, ns, _ = _cache_numel(c)
+    i32, bf = torch.int32, torch.bfloat16
+    rows = a.batch * a.heads * a.q_len
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().wise_prefix_attn(
+        ctypes.byref(c), ctypes.byref(a), _ptr(q, bf, "q", rows * c.head_dim),
+        _ptr(k_pool, bf, "k_pool", npl), _ptr(v_pool, bf, "v_pool", npl),
+        _ptr(tables, i32, "tables", nt), _ptr(lens, i32, "lens", ns),
+        _ptr(seq_ids, i32, "seq_ids", a.batch), _ptr(shared, i32, "shared", a.batch),
+        _ptr(o, bf, "o", rows * c.head_dim), _ptr(lse, torch.float32, "lse", rows),
+        _ptr(workspace, None, "workspace"), ctypes.c_size_t(ws_bytes), _stream(stream)),
+        "wise_prefix_attn")
+
+
+def wise_cache_workspace_bytes(c: wise_cache) -> int:
+    return int(_lib().wise_cache_workspace_bytes(ctypes.byref(c)))
+
+
+def wise_prefix_workspace_bytes(c: wise_cache, a: wise_queries) -> int:
+    return int(_lib().wise_prefix_workspace_bytes(ctypes.byref(c), ctypes.byref(a)))
 
 
 def wise_status_string(status: int) -> str:

@@ -1,0 +1,316 @@
+"""wise_prefix_attn on the GPU against the fp64 definition, row by row: one
+to 128 query rows a key-value head, shared and private pages, empty and one-token
+sequences, lengths at page and tile borders, garbage beyond a sequence."""
+
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from cache_model import attend, bf16_values, up
+from paper_2609_27373_amd.cache import PagedCache
+from parity_util import say
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Batch:
+    """A cache whose unused slots hold NaN, and a batch of queries.  groups: list of (pages shared, [tail lengths]);
+    a tail of None is an empty sequence."""
+
+    def __init__(self, groups, page, d, kv, gq, q_len=1, seed=0, gain=1.0, slots=False, spare=3):
+        g = torch.Generator().manual_seed(seed)
+        rng = random.Random(seed)
+        batch = sum(len(t) for _, t in groups)
+        lens = [0 if x is None else pre * page + x for pre, tails in groups for x in tails]
+        need = sum(pre for pre, _ in groups) + sum(up(x or 0, page) for _, t in groups for x in t)
+        pages, seqs = need + spare, batch + 2
+        cols = max(1, max(up(n, page) for n in lens))
+        order = rng.sample(range(pages), pages)
+        self.ids = rng.sample(range(seqs), batch) if slots else list(range(batch))
+        tables, all_lens, shared, i = np.full((seqs, cols), -1), np.zeros(seqs, int), [], 0
+        for pre, tails in groups:
+            first = [order.pop() for _ in range(pre)]
+            for j, x in enumerate(tails):
+                row = [] if x is None else first + [order.pop() for _ in range(up(x, page))]
+                tables[self.ids[i], :len(row)] = row
+                all_lens[self.ids[i]] = lens[i]
+                shared.append(pre if j else 0)
+                i += 1
+        pool = torch.full((2, pages, kv, page, d), float("nan"), dtype=torch.bfloat16)
+        for s in range(seqs):
+            for p0 in range(0, int(all_lens[s]), page):
+                n = min(page, int(all_lens[s]) - p0)
+                p = int(tables[s, p0 // page])
+                if torch.isnan(pool[0, p, 0, 0, 0]):
+                    pool[:, p, :, :n] = torch.randn((2, kv, n, d), generator=g).to(torch.bfloat16)
+        self.tables, self.lens, self.shared, self.page = tables, all_lens, shared, page
+        self.pool = pool
+        self.q = (gain * torch.randn((batch, kv * gq, q_len, d), generator=g)).to(torch.bfloat16)
+        self.cache = PagedCache(1, pages, page, kv, d, seqs, cols, pool=pool.cuda(), tables=ints(tables.tolist()),
+                                lens=ints(all_lens.tolist()))
+
+    def run(self, shared=True, scale=0.0, out=None):
+        q = self.q.cuda()
+        out = torch.full_like(q, float("nan")) if out is None else out
+        lse = torch.full(q.shape[:3], float("nan"), dtype=torch.float32, device="cuda")
+        self.cache.attend(0, q, out, lse, seq_ids=ints(self.ids), shared=ints(self.shared) if shared else None, scale=scale)
+        torch.cuda.synchronize()
+        return out, lse
+
+    def check(self, out, lse, scale=0.0):
+        f64 = lambda t: bf16_values(t.view(torch.int16).numpy())  # noqa: E731
+        scale = np.float32(scale if scale > 0 else 1 / np.sqrt(self.q.shape[-1])).astype(float)
+        o, z, bound, zb = attend(f64(self.q), f64(self.pool[0]), f64(self.pool[1]), self.tables, self.lens, self.ids, self.page, scale)
+        got, gz = out.float().cpu().numpy().astype(float), lse.cpu().numpy().astype(float)
+        err = np.abs(got - o)
+        assert np.all(err <= bound), f"o: {np.nanmax(err - bound):.3g} past the bound, NaN {np.isnan(got).sum()}"
+        empty = np.isneginf(z)
+        assert np.array_equal(np.isneginf(gz), empty)
+        assert np.all(np.abs(gz[~empty] - z[~empty]) <= zb[~empty])
+        assert np.all(got[empty] == 0)
+
+    def both(self, scale=0.0):
+        for shared in (True, False):
+            self.check(*self.run(shared, scale), scale)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("gq", [1, 4, 7])
+def test_lengths(gpu_lib, page, d, gq):
+    """No prefix: empty, one token, and every side of the page and tile borders."""
+    tails = [None, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 300]
+    b = Batch([(0, tails)], page, d, 2, gq, seed=page + d + gq)
+    b.check(*b.run(False))
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("members", [2, 17, 40])
+def test_shared_prefix(gpu_lib, page, d, members):
+    """One group: 4 query heads a key-value head, so 8, 68 and 160 rows share the prefix."""
+    rng = random.Random(members)
+    b = Batch([(up(200, page), [rng.randint(1, 90) for _ in range(members)])], page, d, 2, 4, seed=page + d + members)
+    b.both()
+
+
+@pytest.mark.parametrize("gq,q_len", [(1, 2), (1, 128), (4, 5), (8, 4), (8, 16), (3, 11), (128, 1), (16, 2), (33, 1), (17, 3)])
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 64), (128, 32)])
+def test_query_rows(gpu_lib, gq, q_len, d, page):
+    """Several tokens a sequence and wide groups of heads; the first tokens of short sequences see nothing."""
+    tails = [1, q_len, q_len + 1, max(1, q_len - 1), 70, 129, None, 40]
+    b = Batch([(0, tails), (up(150, page), [q_len, q_len + 60, q_len + 7])], page, d, 1, gq, q_len, seed=gq * q_len, slots=True)
+    b.both()
+
+
+@pytest.mark.parametrize("d,page", [(64, 32), (96, 16), (128, 128)])
+def test_drafts_longer_than_tails(gpu_lib, d, page):
+    """Queries that reach back into the shared pages: these stay out of what is read once."""
+    b = Batch([(4, [0, 1, 5, 0]), (2, [3, 0])], page, d, 2, 2, q_len=9, seed=5)
+    b.both()
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (96, 32), (128, 64), (128, 128)])
+def test_groups(gpu_lib, d, page):
+    """Several prompts in a batch, single requests between, an empty slot, table rows in another order."""
+    groups = [(3, [5, 60, 1]), (0, [40]), (7, [9] * 12), (0, [None]), (0, [None, 3]), (1, [33, 2]), (12, [100] * 33)]
+    b = Batch(groups, page, d, 3, 2, seed=d + page, slots=True)
+    b.both()
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("heads", [(1, 1), (5, 1), (2, 8)])
+def test_long(gpu_lib, d, heads):
+    """A long key axis split over many work-groups and joined, with and without sharing."""
+    b = Batch([(500, [1, 777, 16]), (0, [9000])], 16, d, *heads, seed=d)
+    b.both()
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 16)])
+def test_many_sequences(gpu_lib, d, page):
+    rng = random.Random(d)
+    b = Batch([(2, [rng.randint(1, 60) for _ in range(300)]), (0, [rng.randint(1, 60) for _ in range(724)])], page, d, 1, 1, seed=d)
+    b.both()
+
+
+@pytest.mark.parametrize("gain,scale", [(60.0, 0.0), (1.0, 3.0), (0.0, 0.0), (1.0, 1e-6)])
+def test_scores(gpu_lib, gain, scale):
+    """Weights on one key, flat weights, a given scale."""
+    b = Batch([(9, [40, 7, 3, 90] * 3), (0, [300])], 32, 128, 2, 4, seed=3, gain=gain)
+    b.both(scale)
+
+
+def test_scores_that_overflow(gpu_lib):
+    """Keys of the largest finite values: scores past the fp32 range below give weight 0, not NaN."""
+    b = Batch([(5, [20, 50, 33])], 16, 64, 1, 4, seed=8)
+    big = torch.finfo(torch.bfloat16).max
+    for s in b.ids:
+        p = int(b.tables[s, int(b.lens[s] - 1) // 16])
+        b.pool[0, p, :, 0] = -big
+    b.q = b.q.abs() + 1
+    b.cache.pool.copy_(b.pool)
+    out, lse = b.run()
+    keep = b.pool.clone()
+    for s in b.ids:                                   # those keys hold no weight: the same without them
+        p = int(b.tables[s, int(b.lens[s] - 1) // 16])
+        b.pool[0, p, :, 0] = -1e4
+    b.check(out, lse)
+    b.pool = keep
+
+
+def test_infinite_keys_and_values(gpu_lib):
+    """An infinite or NaN value makes the rows that see it non-finite in its dim, and no other row or dim."""
+    b = Batch([(3, [30, 40, 50, 60])], 16, 64, 2, 2, q_len=3, seed=9)
+    ref, _ = b.run()
+    p = int(b.tables[b.ids[2], 5])                    # sequence 2's newest full page, private
+    pos = int(b.lens[b.ids[2]]) - 1                   # its newest token: only the last query sees it
+    p, at = int(b.tables[b.ids[2], pos // 16]), pos % 16
+    for bad in (float("inf"), float("nan")):
+        b.cache.pool.copy_(b.pool)
+        b.cache.pool[1, p, 0, at, 7] = bad
+        out, _ = b.run()
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[2, :2, 2, 7] = True                       # kv head 0, last token, dim 7
+        assert not torch.isfinite(out[hit]).any()
+        assert torch.equal(out[~hit], ref[~hit]), bad
+        b.cache.pool.copy_(b.pool)
+        b.cache.pool[0, p, 1, at, 3] = bad if bad != bad else -bad
+        out, _ = b.run()
+        rest = torch.ones_like(out, dtype=torch.bool)
+        rest[2, 2:, 2] = False                        # kv head 1, last token
+        assert torch.equal(out[rest], ref[rest]), bad
+
+
+def test_bad_tables_and_lengths(gpu_lib):
+    """Page ids outside the pool are not read, their positions not attended; lengths past the table and below 0 are cut."""
+    b = Batch([(4, [30, 70, 20, 40]), (0, [100])], 16, 64, 1, 4, seed=4)
+    ids = b.ids
+    b.tables[ids[1], 5], b.tables[ids[3], 4] = b.pool.shape[1], -7
+    b.tables[ids[2], 4] = 2 ** 31 - 1
+    for s in ids[:4]:
+        b.tables[s, 1] = -1                           # inside the shared pages
+    cols = b.tables.shape[1]
+    b.tables[ids[4], 3] = -2 ** 31
+    b.lens[ids[0]] = -5
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    b.cache.lens.copy_(ints(b.lens.tolist()))
+    b.both()
+    full = [s for s in ids if b.tables[s, cols - 1] >= 0][0]
+    b.pool.nan_to_num_(0.5)
+    b.cache.pool.copy_(b.pool)
+    b.lens[full] = cols * 16 + 1000
+    b.cache.lens.copy_(ints(b.lens.tolist()))
+    b.both()
+
+
+def test_repeated_and_foreign_ids(gpu_lib):
+    b = Batch([(2, [30, 5]), (0, [9])], 16, 64, 2, 2, seed=6)
+    b.ids = [b.ids[0], b.ids[0], b.ids[2]]
+    b.shared = [0, 4, -3]
+    b.both()
+    b.ids = [99, b.ids[0], -1]
+    b.shared = [5, 2, 2]
+    b.both()
+
+
+def test_shared_larger_than_it_is(gpu_lib):
+    """shared is cut to what every member of a run holds."""
+    b = Batch([(2, [30, 5, 1])], 16, 64, 2, 2, seed=7)
+    b.shared = [77, 2, 10 ** 9]
+    b.both()
+
+
+def test_rows_are_left_alone(gpu_lib):
+    """Nothing is written behind the batch's rows."""
+    b = Batch([(2, [30, 5, 1] * 5)], 16, 96, 2, 2, seed=7)
+    big = torch.full((b.q.numel() + 4096,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = big[:b.q.numel()].view(b.q.shape)
+    b.check(*b.run(out=out))
+    assert bool((big[b.q.numel():] == 7).all())
+
+
+def test_long_pool(gpu_lib):
+    """Pages past 4 GB of a plane."""
+    d, kv, page = 128, 8, 128
+    pages = 20000                                     # 5.2 GB a plane
+    c = PagedCache(1, pages, page, kv, d, 2, 3, pool=torch.empty((2, pages, kv, page, d), dtype=torch.bfloat16, device="cuda"))
+    c.tables.copy_(ints([[19999, 3, 17001], [19999, 18888, -1]]))
+    c.lens.copy_(ints([300, 200]))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    used = [19999, 3, 17001, 18888]
+    small = torch.randn((2, 4, kv, page, d), generator=g, device="cuda").to(torch.bfloat16)
+    c.pool[:, used] = small
+    q = torch.randn((2, 2 * kv, 1, d), generator=g, device="cuda").to(torch.bfloat16)
+    want = PagedCache(1, 4, page, kv, d, 2, 3, pool=small, tables=ints([[0, 1, 2], [0, 3, -1]]), lens=ints([300, 200]))
+    outs = []
+    for x in (c, want):
+        for sh in (None, ints([0, 1])):
+            outs.append(x.attend(0, q, torch.empty_like(q), shared=sh))
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+    # moves of such pages: the copy of a shared last page, and compaction
+    c.refs.zero_()
+    c.refs[ints(used).long()] = ints([2, 1, 1, 1])
+    live = c.compact()
+    torch.cuda.synchronize()
+    assert int(live) == 4
+    # 3 stays; the others go to 0, 1, 2 in ascending order
+    assert c.tables.cpu().tolist() == [[2, 3, 0], [2, 1, -1]]
+    assert torch.equal(c.pool[:, [2, 3, 0, 1]], small)
+
+
+def test_graph_and_streams(gpu_lib):
+    """Replays of a captured call between eager ones, with lengths changing; calls of two shapes on two streams."""
+    b = Batch([(5, [30, 5, 64, 100] * 9), (0, [200])], 16, 128, 2, 4, seed=11)
+    q, sh, ids = b.q.cuda(), ints(b.shared), ints(b.ids)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device="cuda")
+    eager = [t.clone() for t in b.run()]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.cache.attend(0, q, out, lse, seq_ids=ids, shared=sh)
+    full = b.cache.lens.clone()
+    for rep in range(4):
+        b.cache.lens.copy_(full - 4 * (rep % 2))
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        want = b.run()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        if rep % 2 == 0:
+            assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+    other = Batch([(0, [900, 30])], 64, 64, 3, 1, seed=12)
+    first, second = b.run()[0].clone(), other.run()[0].clone()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    o1, o2, q2 = torch.empty_like(q), torch.empty_like(second), other.q.cuda()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(s1):
+            b.cache.attend(0, q, o1, seq_ids=ids, shared=sh)
+        with torch.cuda.stream(s2):
+            other.cache.attend(0, q2, o2)
+    torch.cuda.synchronize()
+    assert torch.equal(o1, first) and torch.equal(o2, second)
+
+
+def test_after_a_prompt(gpu_lib):
+    """A prompt's keys and values go into the cache and its last token attends: the dense call's last row."""
+    w = gpu_lib
+    n, heads, kv, d = 320, 8, 2, 96
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v = (torch.randn((2, h, n, d), generator=g, device="cuda").to(torch.bfloat16) for h in (heads, kv, kv))
+    o, lse = torch.empty_like(q), torch.empty((2, heads, n), dtype=torch.float32, device="cuda")
+    w.wise_dense_attn_accum(w.make_shape(2, heads, n, d, 64, kv_heads=kv), q, k, v, o, lse)
+    c = PagedCache(1, 30, 32, kv, d, 4, 12)
+    ids = ints([2, 0])
+    c.append(0, k, v, ids, c.reserve(ids, ints([n, n])))
+    last, z = torch.empty((2, heads, 3, d), dtype=torch.bfloat16, device="cuda"), torch.empty((2, heads, 3), device="cuda")
+    c.attend(0, q[:, :, -3:].contiguous(), last, z, seq_ids=ids)
+    torch.cuda.synchronize()
+    # Both are within 2^-8 |o| + 2^-8 A (rounded output, rounded probabilities) of the definition; |v| < 6 gives A < 6.
+    assert (last.float() - o[:, :, -3:].float()).abs().max() <= 2 * (2 ** -8 * 6 + 2 ** -8 * 6)
+    assert (z - lse[:, :, -3:]).abs().max() <= 1e-4
