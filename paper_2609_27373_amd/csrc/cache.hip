@@ -6,16 +6,12 @@
 // lowest free page goes to the first entry that needs one), so one work-group
 // plans it from ballots and prefix sums, and a second launch moves the bytes.
 // Reference counts change by integer atomics: any order gives the same count.
+#include "plan.hpp"
 #include "wise_device.hpp"
 #include "wise_kernels.hpp"
 
 namespace wise {
 namespace {
-
-constexpr int kPlan = 1024;            // threads of a planning work-group
-constexpr int kPlanWaves = kPlan / 64;
-
-__device__ __forceinline__ bool in_range(int x, int n) { return (unsigned)x < (unsigned)n; }
 
 __device__ __forceinline__ int clamp_len(int len, const Cache& c) {
   const int cap = c.max_pages * c.page;
@@ -27,28 +23,6 @@ __device__ __forceinline__ bool any_equal(const int32_t* ids, int n, int x) {
   bool hit = false;
   for (int j = threadIdx.x; j < n; j += blockDim.x) hit |= ids[j] == x;
   return __syncthreads_or(hit);
-}
-
-// Exclusive prefix sum of x over the planning work-group, and the total.
-__device__ int64_t plan_scan(int64_t x, int64_t* total, int64_t* waves) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t s = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)s, o, 64);
-    if (lane >= o) s += y;
-  }
-  __syncthreads();
-  if (lane == 63) waves[wave] = s;
-  __syncthreads();
-  int64_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    before += w < wave ? waves[w] : 0;
-    all += waves[w];
-  }
-  *total = all;
-  return before + s - x;
 }
 
 // The pages of [lo, hi) that are free (kFree) or in use, ascending: page number r
@@ -143,8 +117,8 @@ struct ReserveCopy {
 __global__ void __launch_bounds__(kPlan)
 reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32_t* __restrict__ counts, int32_t* tables,
                     int32_t* lens, int32_t* refs, int32_t* granted, int32_t* list, ReserveCopy* copies) {
-  __shared__ int32_t id_[kPlan], begin_[kPlan], row_[kPlan];
-  __shared__ int64_t first_[kPlan + 1], waves[kPlanWaves];
+  __shared__ int32_t id_[kPlan], begin_[kPlan], row_[kPlan], first_[kPlan];
+  __shared__ int64_t waves[kPlanWaves];
   const int i = threadIdx.x;
   const int s = i < n ? ids[i] : -1, count = i < n ? counts[i] : 0;
   id_[i] = s;
@@ -173,25 +147,17 @@ reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32
   const int64_t first = plan_scan(need, &total, waves);
   const int free_pages = list_pages<true>(refs, 0, c.pages, waves, [&](int r, int p) { list[r] = p; });
   ok = ok && (need == 0 || first + need <= free_pages);
-  // Entries past the first that does not fit need not be considered for the
-  // places: theirs lie past the free pages.
-  first_[i] = first;
+  first_[i] = (int32_t)(first < free_pages ? first : (int64_t)free_pages);   // past them: no place is its
   row_[i] = ok ? s : -1;
   begin_[i] = begin;
-  if (i == 0) first_[kPlan] = total;
   __syncthreads();                     // the list, too, is written
   const int places = (int)(total < free_pages ? total : (int64_t)free_pages);
   for (int k = i; k < places; k += kPlan) {
-    int lo = 0, hi = kPlan;            // the entry whose pages hold place k
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (first_[mid] <= k) lo = mid;
-      else hi = mid;
-    }
-    if (row_[lo] < 0) continue;
+    const int e = plan_entry(first_, k);
+    if (row_[e] < 0) continue;
     const int p = list[k];
     refs[p] = 1;
-    tables[(size_t)row_[lo] * c.max_pages + begin_[lo] + (k - (int)first_[lo])] = p;
+    tables[(size_t)row_[e] * c.max_pages + begin_[e] + (k - first_[e])] = p;
   }
   if (i < n) {
     ReserveCopy r{0, 0, 0, 0};
