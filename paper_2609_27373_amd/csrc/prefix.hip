@@ -16,8 +16,8 @@
 #include <algorithm>
 
 #include "plan.hpp"
-#include "wise_device.hpp"
 #include "wise_kernels.hpp"
+#include "wise_tiles.hpp"
 
 namespace wise {
 namespace {
@@ -29,7 +29,8 @@ struct Piece {
   int32_t table;                       // table row with the segment's pages
   int32_t see;                         // positions that a sequence's first query sees
   int32_t slot;                        // row of the piece's results, key-value head 0, segment row 0; -1: the whole result, written to o
-  int32_t pad[3];
+  int32_t wide;                        // up to kWide rows, for tile_piece
+  int32_t pad[2];
 };
 
 // Where the pieces of a sequence's rows lie: results of row r over piece i of the
@@ -42,6 +43,7 @@ struct Joint {
 
 // Target numbers of work-groups, and the fewest keys of a piece.
 constexpr int kGroups = 2048, kFewKeys = 64;
+constexpr int kWide = 128, kWideGroups = 512, kWideKeys = 256;   // the same for pieces of many rows
 
 struct Space {                         // the workspace
   int32_t* count;
@@ -58,13 +60,18 @@ struct Limits {
 int row_tile(const Cache& c, const Queries& a) { return a.heads / c.kv_heads * a.q_len > 16 ? 32 : 16; }
 
 // A segment of t row tiles and K keys is cut into at most K / C + 1 pieces, and C is
-// at least sum(t K) * kv_heads / kGroups and kFewKeys.
+// at least sum(t K) * kv_heads / groups and the fewest keys of a piece.
 Limits limits(const Cache& c, const Queries& a) {
-  const int64_t rows = (int64_t)a.heads / c.kv_heads * a.q_len, tile = row_tile(c, a), b = a.batch;
-  const int64_t tiles = b * ((rows + tile - 1) / tile) + (b * rows / tile + b / 2);   // own rows, shared rows
-  const int64_t most = ((int64_t)c.max_pages * c.page + kFewKeys - 1) / kFewKeys;     // pieces of a segment
-  const int64_t cut = std::min<int64_t>(kGroups / c.kv_heads + 1 + tiles, tiles * most);
-  return Limits{cut, std::min<int64_t>(tile * (kGroups + c.kv_heads) + 2 * c.kv_heads * b * rows, 2 * c.kv_heads * b * rows * most)};
+  const int64_t rows = (int64_t)a.heads / c.kv_heads * a.q_len, tile = row_tile(c, a), b = a.batch, kv = c.kv_heads;
+  const int64_t cap = (int64_t)c.max_pages * c.page;
+  const int64_t tiles = b * ((rows + tile - 1) / tile) + b / 2;                       // own rows, shared ones of one tile
+  const int64_t most = (cap + kFewKeys - 1) / kFewKeys;                               // pieces of a segment
+  const int64_t wide_tiles = std::min<int64_t>(b / 2, b * rows / tile) + b * rows / kWide;
+  const int64_t wide_most = (cap + kWideKeys - 1) / kWideKeys;
+  const int64_t few = std::min<int64_t>(kGroups / kv + 1 + tiles, tiles * most);
+  const int64_t wide = std::min<int64_t>(kWideGroups / kv + 1 + wide_tiles, wide_tiles * wide_most);
+  return Limits{few + wide, std::min<int64_t>(tile * (kGroups + kv) + 2 * kv * b * rows, 2 * kv * b * rows * most) +
+                                std::min<int64_t>(kWide * (kWideGroups + kv) + kv * b * rows, kv * b * rows * wide_most)};
 }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -104,7 +111,7 @@ __global__ void __launch_bounds__(kPlan)
 plan_kernel(Cache c, Queries a, int tile, int64_t most, const int32_t* __restrict__ tables_ids, const int32_t* __restrict__ lens,
             const int32_t* __restrict__ shared, int32_t* __restrict__ count, Joint* __restrict__ joint, Piece* __restrict__ piece) {
   __shared__ int32_t members[kPlan], min_pages[kPlan], min_see[kPlan];
-  __shared__ int32_t first_[kPlan], id_[kPlan], len_[kPlan], own_len[kPlan], own_slot[kPlan], pre_slot[kPlan], pre_pieces[kPlan],
+  __shared__ int32_t first_[kPlan], wide_first_[kPlan], id_[kPlan], len_[kPlan], own_len[kPlan], own_slot[kPlan], pre_slot[kPlan], pre_pieces[kPlan],
       pre_len[kPlan];
   __shared__ int64_t waves[kPlanWaves];
   __shared__ int32_t wave_start[kPlanWaves];
@@ -143,19 +150,26 @@ plan_kernel(Cache c, Queries a, int tile, int64_t most, const int32_t* __restric
   const int own = len - pre;
   const int own_tiles = up_to(rows, tile);
   const bool leads = live && b == start && pre > 0;
-  const int pre_rows = leads ? n * rows : 0, pre_tiles = up_to(pre_rows, tile);
-  int64_t keys;
-  plan_scan((int64_t)own_tiles * own + (int64_t)pre_tiles * pre, &keys, waves);
-  const int64_t even = (keys * c.kv_heads + kGroups - 1) / kGroups;
-  const int chunk = (int)min(max(even, (int64_t)kFewKeys), (int64_t)1 << 30);
+  const int pre_rows = leads ? n * rows : 0;
+  const bool wide = pre_rows > tile;
+  const int pre_tiles = up_to(pre_rows, wide ? kWide : tile);
+  int64_t keys, wide_keys;
+  plan_scan((int64_t)own_tiles * own + (wide ? 0 : (int64_t)pre_tiles * pre), &keys, waves);
+  plan_scan(wide ? (int64_t)pre_tiles * pre : 0, &wide_keys, waves);
+  auto even = [&](int64_t sum, int groups, int least) {
+    return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
+  };
+  const int chunk = even(keys, kGroups, kFewKeys);
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  cut_keys(leads ? pre : 0, chunk, 64, pre_n, pre_l);
+  cut_keys(leads ? pre : 0, wide ? even(wide_keys, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
-  int64_t all, slots;
-  const int64_t first = plan_scan((int64_t)own_n * own_tiles + (int64_t)pre_n * pre_tiles, &all, waves);
+  int64_t few, wides, slots;
+  const int64_t first = plan_scan((int64_t)own_n * own_tiles + (wide ? 0 : (int64_t)pre_n * pre_tiles), &few, waves);
+  const int64_t wide_first = plan_scan(wide ? (int64_t)pre_n * pre_tiles : 0, &wides, waves);
   const int64_t slot = plan_scan((done ? 0 : (int64_t)own_n * c.kv_heads * rows) + (int64_t)pre_n * c.kv_heads * pre_rows, &slots, waves);
   first_[b] = (int)first;
+  wide_first_[b] = (int)wide_first;
   id_[b] = id;
   len_[b] = len;
   own_len[b] = own_l;
@@ -168,17 +182,25 @@ plan_kernel(Cache c, Queries a, int tile, int64_t most, const int32_t* __restric
   __syncthreads();
   if (live)
     joint[b] = Joint{pre_slot[start], pre > 0 ? pre_pieces[start] : 0, n * rows, (b - start) * rows, own_slot[b], own_n, done, 0};
-  if (b == 0) *count = (int)min(all, most);
-  for (int k = b; k < (int)min(all, most); k += kPlan) {
-    const int e = plan_entry(first_, k);
-    int j = k - first_[e];
-    const int p_rows = pre_pieces[e] > 0 ? members[e] * rows : 0, p_tiles = up_to(p_rows, tile), p_all = pre_pieces[e] * p_tiles;
+  const int all = (int)min(few + wides, most);
+  if (b == 0) *count = all;
+  // Pieces of few rows wait for memory, those of many for the matrix cores: the
+  // two kinds alternate, so that a CU holds both.
+  const int both = 2 * (int)min(few, wides);
+  for (int k = b; k < all; k += kPlan) {
+    const bool is_wide = k < both ? k % 2 == 0 : wides > few;
+    const int in_kind = k < both ? k / 2 : k - both / 2;
+    const int e = plan_entry(is_wide ? wide_first_ : first_, in_kind);
+    int j = in_kind - (is_wide ? wide_first_ : first_)[e];
+    const int p_rows = pre_pieces[e] > 0 ? members[e] * rows : 0;
+    const int p_tile = is_wide ? kWide : tile, p_tiles = up_to(p_rows, p_tile), p_all = is_wide || p_rows <= tile ? pre_pieces[e] * p_tiles : 0;
     Piece p;
     p.first = e;
+    p.wide = is_wide;
     if (j < p_all) {
       const int i = j / p_tiles, t = j % p_tiles;
       p.seg_rows = p_rows;
-      p.row0 = t * tile;
+      p.row0 = t * p_tile;
       p.k0 = i * pre_len[e];
       p.k1 = min(p.k0 + pre_len[e], min_pages[e]);
       p.see = 0x7fffffff - a.q_len;
@@ -193,9 +215,9 @@ plan_kernel(Cache c, Queries a, int tile, int64_t most, const int32_t* __restric
       p.see = len_[e] - a.q_len + 1;
       p.slot = own_slot[e] < 0 ? -1 : own_slot[e] + i * c.kv_heads * rows;
     }
-    p.rows = min(tile, p.seg_rows - p.row0);
+    p.rows = min(is_wide ? kWide : tile, p.seg_rows - p.row0);
     p.table = id_[e];
-    p.pad[0] = p.pad[1] = p.pad[2] = 0;
+    p.pad[0] = p.pad[1] = 0;
     piece[k] = p;
   }
 }
@@ -466,14 +488,158 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   }
 }
 
-template <int D, int NT>
+// ---------------------------------------------------------------------------
+// A piece of up to 128 rows, all of which see all its keys (whole tiles of
+// 64): the software pipeline of the dense kernel (WaveRows::step), four waves
+// of 32 rows over rings of two K and two V tiles in LDS.  A wave copies 16
+// consecutive keys of a tile, which lie in one page.
+// ---------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, int kh, char* smem) {
+  using G = Geo<D>;
+  constexpr int kT = Swizzle<D>::kTile, kC = TileCopy<D, 4>::kPer;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, page = x.c.page;
+  const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
+  const int tiles = (p.k1 - p.k0) / kKeyTile;
+  // Page ids of this wave's keys: lane i has the one of tile 64 u + i, of stretch u and the next one.
+  auto load_ids = [&](int u) {
+    const int key = p.k0 + (64 * u + lane) * kKeyTile + 16 * wave;
+    return key < p.k1 ? table[key / page] : 0;
+  };
+  int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
+  WaveRows<D> w;
+  w.reset();
+  {
+    const int r = p.row0 + min(32 * wave + (lane & 31), p.rows - 1);
+    const int b = p.first + r / rows;
+    const uint16_t* row = x.q + (((size_t)b * x.c.kv_heads + kh) * rows + r % rows) * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
+  }
+  TileCopy<D, 4> cp;
+  ReadAddr<D> ra;
+  cp.init(wave, lane);
+  ra.init(lane);
+#pragma unroll
+  for (int i = 0; i < kC; ++i) {                    // offsets from the wave's first key
+    cp.ko[i] -= 16 * wave * Swizzle<D>::kRow;
+    cp.vo[i] -= 16 * wave * Swizzle<D>::kRow;
+  }
+  const uint32_t lk = lds_address(smem), lv = lk + 2 * kT;
+  const char* sk = smem;
+  const char* sv = smem + 2 * kT;
+  auto source = [&](const uint16_t* pool, int it) { // this wave's keys of tile it
+    const int id = __builtin_amdgcn_readlane(it >> 6 == stretch ? ids : next_ids, it & 63);
+    const int key = p.k0 + it * kKeyTile + 16 * wave;
+    return buffer_words(pool + (((size_t)id * x.c.kv_heads + kh) * page + (key & (page - 1))) * D);
+  };
+  auto copy_k = [&](u32x4_t from, int it, int i) { cp.k1(from, 0, lk + (it & 1) * kT, wave, i); };
+  auto copy_v = [&](u32x4_t from, int it, int i) { cp.v1(from, 0, lv + (it & 1) * kT, wave, i); };
+  {
+    const u32x4_t k0 = source(x.kp, 0), v0 = source(x.vp, 0);
+#pragma unroll
+    for (int i = 0; i < kC; ++i) copy_k(k0, 0, i);
+#pragma unroll
+    for (int i = 0; i < kC; ++i) copy_v(v0, 0, i);
+    if (tiles > 1) {
+      const u32x4_t k1 = source(x.kp, 1);
+#pragma unroll
+      for (int i = 0; i < kC; ++i) copy_k(k1, 1, i);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < G::kDChunks; ++i) asm volatile("" : "+v"(w.qf[i]));
+  wait_copies<0>();
+  __syncthreads();
+  const bool active = 32 * wave < p.rows;
+  f32x16_t s0[2], s1[2];
+  float mx = 0.f;
+  if (active) w.template step<2, true, false, 0>(sk, sv, ra, lane, x.sc, s1, s0, mx, [](auto, int) {}, [](f32x16_t*) {});
+  __syncthreads();                                  // K(0) read by every wave: K(2) may take its place
+  // Step `it`: S^T of tile it + 1, softmax and PV of tile it; V(it + 1) and K(it + 2)
+  // go where V(it - 1) and K(it) were.  At its end both have landed.
+  auto fused = [&](int it, f32x16_t sc[2], f32x16_t sn[2]) {
+    const int b = it & 1;
+    if (it >> 6 != stretch) {
+      stretch = it >> 6;
+      ids = next_ids;
+      next_ids = load_ids(stretch + 1);
+    }
+    const u32x4_t fv = source(x.vp, it + 1), fk = source(x.kp, min(it + 2, tiles - 1));
+    const bool more = it + 2 < tiles;
+    auto copy = [&](int i) {
+      if (i < kC) copy_v(fv, it + 1, i);
+      else if (more) copy_k(fk, it + 2, i - kC);
+    };
+    if (active) {
+      w.template step<2, true, true, 0>(sk + (b ^ 1) * kT, sv + b * kT, ra, lane, x.sc, sc, sn, mx,
+                                        [&](auto n, int j) {
+                                          constexpr int kGap = std::max(1, (decltype(n)::value * 5 / 8 - 2) / (2 * kC));
+                                          if (j >= 2 && (j - 2) % kGap == 0 && (j - 2) / kGap < 2 * kC) copy((j - 2) / kGap);
+                                        },
+                                        [](f32x16_t*) {});
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * kC; ++i) copy(i);
+    }
+    wait_copies<0>();
+    __syncthreads();
+  };
+  int it = 0;
+  for (; it + 2 < tiles; it += 2) {
+    fused(it, s0, s1);
+    fused(it + 1, s1, s0);
+  }
+  if (it + 1 < tiles) {
+    fused(it, s0, s1);
+    s0[0] = s1[0];
+    s0[1] = s1[1];
+    ++it;
+  }
+  if (!active) return;
+  w.template step<2, false, true, 0>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
+  const float lt = pair_sum(w.l);
+  const int q = 32 * wave + (lane & 31), h = lane >> 5;
+  if (q >= p.rows) return;
+  const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + q;
+#pragma unroll
+  for (int t = 0; t < G::kDTiles; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(f32x4_t*)(x.part + at * D + 32 * t + 8 * j + 4 * h) =
+          f32x4_t{w.o[t][4 * j], w.o[t][4 * j + 1], w.o[t][4 * j + 2], w.o[t][4 * j + 3]};
+  if (h == 0) x.ml[at] = float2{w.m, lt};
+}
+
+template <int D, int NT, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 piece_kernel(Args x) {
-  __shared__ __attribute__((aligned(16))) float lds[4 * 16 * NT * (D + 4) + 2 * 4 * 16 * NT];
+  constexpr int kJoin = 4 * 16 * NT * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   const int i = blockIdx.x / x.c.kv_heads, kh = blockIdx.x % x.c.kv_heads;
   if (i >= *x.count) return;
   const Piece p = x.piece[i];
-  stream_piece<D, NT>(x, p, kh, lds);
+  if constexpr (kShared) {
+    bool whole = false;
+    if (p.wide) {                                   // every page id of the piece names a page
+      const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
+      bool bad = false;
+      for (int j = p.k0 / x.c.page + threadIdx.x; j <= (p.k1 - 1) / x.c.page; j += 256) bad |= !in_range(table[j], x.c.pages);
+      whole = !__syncthreads_or(bad);
+      if (whole) tile_piece<D>(x, p, kh, smem);
+    }
+    if (whole) return;
+    // A few rows, or, where a page is missing, many a few at a time.
+    Piece s = p;
+    for (int r = 0; r < p.rows; r += 16 * NT) {
+      s.row0 = p.row0 + r;
+      s.rows = min(16 * NT, p.rows - r);
+      stream_piece<D, NT>(x, s, kh, (float*)smem);
+    }
+  } else {
+    stream_piece<D, NT>(x, p, kh, (float*)smem);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -533,8 +699,10 @@ join_kernel(Args x, const Joint* __restrict__ joint, int64_t all) {
 }
 
 template <int D, int NT>
-hipError_t launch(const Args& x, const Joint* joint, int64_t pieces, hipStream_t st) {
-  piece_kernel<D, NT><<<(unsigned)(pieces * x.c.kv_heads), 256, 0, st>>>(x);
+hipError_t launch(const Args& x, const Joint* joint, bool shared, int64_t pieces, hipStream_t st) {
+  const unsigned grid = (unsigned)(pieces * x.c.kv_heads);
+  if (shared) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
+  else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)x.a.batch * x.a.heads * x.a.q_len;
@@ -559,12 +727,12 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
   const Args x{c, a, a.scale * kLog2e, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, tables, s.count, s.piece, s.ml,
                s.part, (uint16_t*)o, lse};
   switch (c.head_dim + tile) {
-    case 64 + 16: return launch<64, 1>(x, s.joint, l.pieces, st);
-    case 96 + 16: return launch<96, 1>(x, s.joint, l.pieces, st);
-    case 128 + 16: return launch<128, 1>(x, s.joint, l.pieces, st);
-    case 64 + 32: return launch<64, 2>(x, s.joint, l.pieces, st);
-    case 96 + 32: return launch<96, 2>(x, s.joint, l.pieces, st);
-    default: return launch<128, 2>(x, s.joint, l.pieces, st);
+    case 64 + 16: return launch<64, 1>(x, s.joint, shared != nullptr, l.pieces, st);
+    case 96 + 16: return launch<96, 1>(x, s.joint, shared != nullptr, l.pieces, st);
+    case 128 + 16: return launch<128, 1>(x, s.joint, shared != nullptr, l.pieces, st);
+    case 64 + 32: return launch<64, 2>(x, s.joint, shared != nullptr, l.pieces, st);
+    case 96 + 32: return launch<96, 2>(x, s.joint, shared != nullptr, l.pieces, st);
+    default: return launch<128, 2>(x, s.joint, shared != nullptr, l.pieces, st);
   }
 }
 
