@@ -43,6 +43,7 @@ class PagedCache:
         self.lens = self._own(lens, (seqs,), torch.int32, "lens", lambda s: torch.zeros(s, **i32))
         self.refs = self._own(refs, (pages,), torch.int32, "refs", lambda s: torch.zeros(s, **i32))
         self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        self._planes = [self.pool[i] for i in range(2 * layers)]
         self._attend = {}
 
     @staticmethod
@@ -87,7 +88,7 @@ class PagedCache:
         """The planes of one layer: (keys, values), [pages][kv_heads][page][head_dim]."""
         if not 0 <= layer < self.shape.planes // 2:
             raise ValueError(f"layer {layer} of {self.shape.planes // 2}")
-        return self.pool[2 * layer], self.pool[2 * layer + 1]
+        return self._planes[2 * layer], self._planes[2 * layer + 1]
 
     def compact(self, live=None):
         """Moves the pages in use to the front of the pool; returns their number (int32 [1], on the device)."""

@@ -153,7 +153,7 @@ reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32
   __syncthreads();                     // the list, too, is written
   const int places = (int)(total < free_pages ? total : (int64_t)free_pages);
   for (int k = i; k < places; k += kPlan) {
-    const int e = plan_entry(first_, k);
+    const int e = plan_entry<kPlan>(first_, k);
     if (row_[e] < 0) continue;
     const int p = list[k];
     refs[p] = 1;

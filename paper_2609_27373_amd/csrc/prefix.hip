@@ -42,8 +42,34 @@ struct Joint {
 };
 
 // Target numbers of work-groups, and the fewest keys of a piece.
-constexpr int kGroups = 2048, kFewKeys = 64;
-constexpr int kWide = 128, kWideGroups = 512, kWideKeys = 256;   // the same for pieces of many rows
+#ifndef GR
+#define GR 1024
+#endif
+#ifndef FK
+#define FK 128
+#endif
+#ifndef WG
+#define WG 256
+#endif
+#ifndef WK
+#define WK 768
+#endif
+constexpr int kGroups = GR, kFewKeys = FK;
+#ifndef MK
+#define MK 512
+#endif
+#ifndef WR
+#define WR 64
+#endif
+constexpr int kWide = 128, kWideGroups = WG, kWideKeys = WK;   // the same for pieces of many rows
+constexpr int kPreTile = 32, kWideRows = WR;   // shared pages: rows of a piece of few rows, and of a segment up to which they are few
+
+// Who plans: nobody (every sequence is one piece), every work-group, a launch before.
+enum { kWhole, kOwnPlan, kPlanned };
+#ifndef WHOLE
+#define WHOLE 512
+#endif
+constexpr int kWholeKeys = WHOLE;      // most keys that are never cut
 
 struct Space {                         // the workspace
   int32_t* count;
@@ -64,13 +90,13 @@ int row_tile(const Cache& c, const Queries& a) { return a.heads / c.kv_heads * a
 Limits limits(const Cache& c, const Queries& a) {
   const int64_t rows = (int64_t)a.heads / c.kv_heads * a.q_len, tile = row_tile(c, a), b = a.batch, kv = c.kv_heads;
   const int64_t cap = (int64_t)c.max_pages * c.page;
-  const int64_t tiles = b * ((rows + tile - 1) / tile) + b / 2;                       // own rows, shared ones of one tile
+  const int64_t tiles = b * ((rows + tile - 1) / tile) + b * rows / kPreTile + b / 2;   // own rows, shared ones
   const int64_t most = (cap + kFewKeys - 1) / kFewKeys;                               // pieces of a segment
-  const int64_t wide_tiles = std::min<int64_t>(b / 2, b * rows / tile) + b * rows / kWide;
+  const int64_t wide_tiles = std::min<int64_t>(b / 2, b * rows / kWideRows) + b * rows / kWide;
   const int64_t wide_most = (cap + kWideKeys - 1) / kWideKeys;
   const int64_t few = std::min<int64_t>(kGroups / kv + 1 + tiles, tiles * most);
   const int64_t wide = std::min<int64_t>(kWideGroups / kv + 1 + wide_tiles, wide_tiles * wide_most);
-  return Limits{few + wide, std::min<int64_t>(tile * (kGroups + kv) + 2 * kv * b * rows, 2 * kv * b * rows * most) +
+  return Limits{few + wide, std::min<int64_t>(kPreTile * (kGroups + kv) + 2 * kv * b * rows, 2 * kv * b * rows * most) +
                                 std::min<int64_t>(kWide * (kWideGroups + kv) + kv * b * rows, kv * b * rows * wide_most)};
 }
 
@@ -93,12 +119,41 @@ size_t space_bytes(const Cache& c, const Queries& a, void* ws, Space* s) {
   return at;
 }
 
-// ---------------------------------------------------------------------------
-// Plan: a thread a sequence.
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ int up_to(int64_t x, int y) { return (int)((x + y - 1) / y); }
+struct Args {
+  Cache c;
+  Queries a;
+  float sc;                            // scale * log2(e)
+  int tile;                            // rows of a piece of few rows
+  int mode;                            // kWhole, kOwnPlan or kPlanned
+  int most;                            // pieces that the workspace holds
+  const uint16_t *q, *kp, *vp;
+  const int32_t *tables, *lens, *ids, *shared;
+  int32_t* count;
+  Joint* joint;
+  Piece* piece;
+  float2* ml;
+  float* part;
+  uint16_t* o;
+  float* lse;
+};
 
-// Pieces of K keys when a piece should hold about `chunk`, and their even length.
+// ---------------------------------------------------------------------------
+// Plan: a thread a sequence.  Up to 256 sequences every work-group plans for
+// itself (its own piece is all it needs), which costs it less than a launch of
+// its own costs the call; more are planned by one group of 1024 threads.
+// ---------------------------------------------------------------------------
+template <int kN>
+struct Plan {                          // LDS
+  int32_t members[kN], pre_keys[kN], see[kN], first[kN], wide_first[kN], id[kN], len[kN], own_len[kN], own_slot[kN], pre_slot[kN],
+      pre_pieces[kN], pre_len[kN];
+  int64_t wave_keys[kN / 64][2];
+  int32_t wave_sum[kN / 64][3], wave_start[kN / 64];
+};
+
+__device__ __forceinline__ int up_to(int64_t x, int y) { return (int)((x + y - 1) / y); }
+__device__ __forceinline__ int up_to(int x, int y) { return (int)(((uint32_t)x + y - 1) / (uint32_t)y); }
+
+// Pieces of `keys` keys when a piece should hold about `chunk`, and their even length.
 __device__ __forceinline__ void cut_keys(int keys, int chunk, int unit, int& pieces, int& len) {
   pieces = 0;
   len = unit;
@@ -107,119 +162,185 @@ __device__ __forceinline__ void cut_keys(int keys, int chunk, int unit, int& pie
   pieces = up_to(keys, len);
 }
 
-__global__ void __launch_bounds__(kPlan)
-plan_kernel(Cache c, Queries a, int tile, int64_t most, const int32_t* __restrict__ tables_ids, const int32_t* __restrict__ lens,
-            const int32_t* __restrict__ shared, int32_t* __restrict__ count, Joint* __restrict__ joint, Piece* __restrict__ piece) {
-  __shared__ int32_t members[kPlan], min_pages[kPlan], min_see[kPlan];
-  __shared__ int32_t first_[kPlan], wide_first_[kPlan], id_[kPlan], len_[kPlan], own_len[kPlan], own_slot[kPlan], pre_slot[kPlan], pre_pieces[kPlan],
-      pre_len[kPlan];
-  __shared__ int64_t waves[kPlanWaves];
-  __shared__ int32_t wave_start[kPlanWaves];
+__device__ __forceinline__ int known_len(const Args& x, int id) {
+  return in_range(id, x.c.seqs) ? min(max(x.lens[id], 0), x.c.max_pages * x.c.page) : 0;
+}
+
+// Runs and pieces of all sequences: few and wides are the numbers of pieces of
+// either kind per key-value head.  Writes x.joint if `write`.
+template <int kN>
+__device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int& wides) {
   const int b = threadIdx.x, lane = b & 63, wave = b >> 6;
+  const Cache& c = x.c;
+  const Queries& a = x.a;
   const bool live = b < a.batch;
-  const int rows = a.heads / c.kv_heads * a.q_len;
-  const int id = !live ? -1 : tables_ids ? tables_ids[b] : b;
-  const bool known = in_range(id, c.seqs);
-  const int cap = c.max_pages * c.page;
-  const int len = known ? min(max(lens[id], 0), cap) : 0;
-  const int see = len - a.q_len + 1;
-  const int sh = live && b > 0 && shared ? shared[b] : 0;
-  // Runs: a sequence belongs to the last start at or before it.
-  int start = sh <= 0 ? b : 0;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(start, o, 64);
-    if (lane >= o) start = max(start, y);
+  const int rows = a.heads / c.kv_heads * a.q_len, tile = x.tile;
+  const int id = !live ? -1 : x.ids ? x.ids[b] : b;
+  const int sh = live && b > 0 && x.shared ? x.shared[b] : 0;
+  const int len = known_len(x, id), see = len - a.q_len + 1;
+  int start = b, n = 1, pre = 0;
+  if (x.shared != nullptr) {
+    // Runs: a sequence belongs to the last start at or before it.
+    start = wave_scan_max(sh <= 0 ? b : 0);
+    if (lane == 63) s.wave_start[wave] = start;
+    s.members[b] = 0;
+    s.pre_keys[b] = s.see[b] = 0x7fffffff;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) start = max(start, s.wave_start[w]);
+    if (live) {
+      atomicAdd(&s.members[start], 1);
+      atomicMin(&s.see[start], see);
+      if (b != start) atomicMin(&s.pre_keys[start], sh);
+    }
+    __syncthreads();
+    // What the run reads once: whole pages that every query sees, in whole
+    // tiles of 64 keys (so that no piece of them needs a mask).
+    n = s.members[start];
+    if (n > 1) pre = (min(s.pre_keys[start], max(s.see[start], 0) / c.page) * c.page) & ~63;
   }
-  if (lane == 63) wave_start[wave] = start;
-  members[b] = 0;
-  min_pages[b] = min_see[b] = 0x7fffffff;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) start = max(start, wave_start[w]);
-  if (live) {
-    atomicAdd(&members[start], 1);
-    atomicMin(&min_see[start], see);
-    if (b != start) atomicMin(&min_pages[start], sh);
-  }
-  __syncthreads();
-  // What the run reads once: whole pages that every query sees, in whole
-  // tiles of 64 keys (so that no piece of them needs a mask).
-  const int n = members[start];
-  int pre = 0;
-  if (n > 1) pre = (min(min_pages[start], max(min_see[start], 0) / c.page) * c.page) & ~63;
-  const int own = len - pre;
-  const int own_tiles = up_to(rows, tile);
+  const int own = len - pre, own_tiles = up_to(rows, tile);
   const bool leads = live && b == start && pre > 0;
   const int pre_rows = leads ? n * rows : 0;
-  const bool wide = pre_rows > tile;
-  const int pre_tiles = up_to(pre_rows, wide ? kWide : tile);
-  int64_t keys, wide_keys;
-  plan_scan((int64_t)own_tiles * own + (wide ? 0 : (int64_t)pre_tiles * pre), &keys, waves);
-  plan_scan(wide ? (int64_t)pre_tiles * pre : 0, &wide_keys, waves);
+  const bool wide = pre_rows > kWideRows;
+  const int pre_tiles = up_to(pre_rows, wide ? kWide : kPreTile);
+  int64_t k0 = (int64_t)own_tiles * own + (wide ? 0 : (int64_t)pre_tiles * pre), k1 = wide ? (int64_t)pre_tiles * pre : 0;
+  k0 = wave_total(k0);
+  k1 = x.shared != nullptr ? wave_total(k1) : 0;
+  if (lane == 0) {
+    s.wave_keys[wave][0] = k0;
+    s.wave_keys[wave][1] = k1;
+  }
+  __syncthreads();
+  k0 = k1 = 0;
+  for (int w = 0; w < kN / 64; ++w) {
+    k0 += s.wave_keys[w][0];
+    k1 += s.wave_keys[w][1];
+  }
   auto even = [&](int64_t sum, int groups, int least) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
-  const int chunk = even(keys, kGroups, kFewKeys);
+  const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), MK));
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  cut_keys(leads ? pre : 0, wide ? even(wide_keys, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
+  cut_keys(leads ? pre : 0, wide ? even(k1, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
-  int64_t few, wides, slots;
-  const int64_t first = plan_scan((int64_t)own_n * own_tiles + (wide ? 0 : (int64_t)pre_n * pre_tiles), &few, waves);
-  const int64_t wide_first = plan_scan(wide ? (int64_t)pre_n * pre_tiles : 0, &wides, waves);
-  const int64_t slot = plan_scan((done ? 0 : (int64_t)own_n * c.kv_heads * rows) + (int64_t)pre_n * c.kv_heads * pre_rows, &slots, waves);
-  first_[b] = (int)first;
-  wide_first_[b] = (int)wide_first;
-  id_[b] = id;
-  len_[b] = len;
-  own_len[b] = own_l;
-  pre_slot[b] = (int)slot;
-  own_slot[b] = done ? -1 : (int)(slot + (int64_t)pre_n * c.kv_heads * pre_rows);
-  pre_pieces[b] = pre_n;
-  pre_len[b] = pre_l;
-  // From here on: keys of the run's shared pages.
-  min_pages[b] = pre;
+  // Prefix sums: pieces of few rows, of many, rows of results.
+  const int mine[3] = {own_n * own_tiles + (wide ? 0 : pre_n * pre_tiles), wide ? pre_n * pre_tiles : 0,
+                       (done ? 0 : own_n * c.kv_heads * rows) + pre_n * c.kv_heads * pre_rows};
+  int sum[3] = {wave_scan_add(mine[0]), x.shared != nullptr ? wave_scan_add(mine[1]) : 0, wave_scan_add(mine[2])};
+  if (lane == 63)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s.wave_sum[wave][i] = sum[i];
   __syncthreads();
-  if (live)
-    joint[b] = Joint{pre_slot[start], pre > 0 ? pre_pieces[start] : 0, n * rows, (b - start) * rows, own_slot[b], own_n, done, 0};
-  const int all = (int)min(few + wides, most);
-  if (b == 0) *count = all;
-  // Pieces of few rows wait for memory, those of many for the matrix cores: the
-  // two kinds alternate, so that a CU holds both.
-  const int both = 2 * (int)min(few, wides);
-  for (int k = b; k < all; k += kPlan) {
-    const bool is_wide = k < both ? k % 2 == 0 : wides > few;
-    const int in_kind = k < both ? k / 2 : k - both / 2;
-    const int e = plan_entry(is_wide ? wide_first_ : first_, in_kind);
-    int j = in_kind - (is_wide ? wide_first_ : first_)[e];
-    const int p_rows = pre_pieces[e] > 0 ? members[e] * rows : 0;
-    const int p_tile = is_wide ? kWide : tile, p_tiles = up_to(p_rows, p_tile), p_all = is_wide || p_rows <= tile ? pre_pieces[e] * p_tiles : 0;
-    Piece p;
-    p.first = e;
-    p.wide = is_wide;
-    if (j < p_all) {
-      const int i = j / p_tiles, t = j % p_tiles;
-      p.seg_rows = p_rows;
-      p.row0 = t * p_tile;
-      p.k0 = i * pre_len[e];
-      p.k1 = min(p.k0 + pre_len[e], min_pages[e]);
-      p.see = 0x7fffffff - a.q_len;
-      p.slot = pre_slot[e] + i * c.kv_heads * p_rows;
-    } else {
-      j -= p_all;
-      const int i = j / own_tiles, t = j % own_tiles;
-      p.seg_rows = rows;
-      p.row0 = t * tile;
-      p.k0 = min_pages[e] + i * own_len[e];
-      p.k1 = min(p.k0 + own_len[e], len_[e]);
-      p.see = len_[e] - a.q_len + 1;
-      p.slot = own_slot[e] < 0 ? -1 : own_slot[e] + i * c.kv_heads * rows;
-    }
-    p.rows = min(is_wide ? kWide : tile, p.seg_rows - p.row0);
-    p.table = id_[e];
-    p.pad[0] = p.pad[1] = 0;
-    piece[k] = p;
+  few = wides = 0;
+  for (int w = 0; w < kN / 64; ++w) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sum[i] += w < wave ? s.wave_sum[w][i] : 0;
+    few += s.wave_sum[w][0];
+    wides += s.wave_sum[w][1];
   }
+  s.first[b] = sum[0] - mine[0];
+  s.wide_first[b] = sum[1] - mine[1];
+  s.id[b] = id;
+  s.len[b] = len;
+  s.own_len[b] = own_l;
+  s.pre_slot[b] = sum[2] - mine[2];
+  s.own_slot[b] = done ? -1 : sum[2] - mine[2] + pre_n * c.kv_heads * pre_rows;
+  s.pre_pieces[b] = pre_n;
+  s.pre_len[b] = pre_l;
+  if (x.shared == nullptr) s.members[b] = 1;
+  s.pre_keys[b] = pre;
+  __syncthreads();
+  if (write && live)
+    x.joint[b] = Joint{s.pre_slot[start], pre > 0 ? s.pre_pieces[start] : 0, n * rows, (b - start) * rows, s.own_slot[b], own_n, done, 0};
+}
+
+// Piece k of a plan: those of many rows first.
+template <int kN>
+__device__ Piece piece_at(const Args& x, const Plan<kN>& s, int wides, int k) {
+  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, kv = x.c.kv_heads;
+  Piece p;
+  p.wide = k < wides;
+  const int32_t* first = p.wide ? s.wide_first : s.first;
+  int j = p.wide ? k : k - wides;
+  const int e = plan_entry<kN>(first, j);
+  j -= first[e];
+  const int pre_rows = s.pre_pieces[e] > 0 ? s.members[e] * rows : 0;
+  int tile = p.wide ? kWide : kPreTile;
+  const int pre_tiles = up_to(pre_rows, tile), pre_all = p.wide || pre_rows <= kWideRows ? s.pre_pieces[e] * pre_tiles : 0;
+  p.first = e;
+  p.table = s.id[e];
+  if (j < pre_all) {
+    const int i = (uint32_t)j / (uint32_t)pre_tiles;
+    p.seg_rows = pre_rows;
+    p.row0 = (j - i * pre_tiles) * tile;
+    p.k0 = i * s.pre_len[e];
+    p.k1 = min(p.k0 + s.pre_len[e], s.pre_keys[e]);
+    p.see = 0x7fffffff - x.a.q_len;
+    p.slot = s.pre_slot[e] + i * kv * pre_rows;
+  } else {
+    j -= pre_all;
+    tile = x.tile;
+    const int own_tiles = up_to(rows, tile), i = (uint32_t)j / (uint32_t)own_tiles;
+    p.seg_rows = rows;
+    p.row0 = (j - i * own_tiles) * tile;
+    p.k0 = s.pre_keys[e] + i * s.own_len[e];
+    p.k1 = min(p.k0 + s.own_len[e], s.len[e]);
+    p.see = s.len[e] - x.a.q_len + 1;
+    p.slot = s.own_slot[e] < 0 ? -1 : s.own_slot[e] + i * kv * rows;
+  }
+  p.rows = min(tile, p.seg_rows - p.row0);
+  p.pad[0] = p.pad[1] = 0;
+  return p;
+}
+
+__global__ void __launch_bounds__(kPlan)
+plan_kernel(Args x) {
+  __shared__ Plan<kPlan> s;
+  int few, wides;
+  make_plan<kPlan>(x, s, true, few, wides);
+  const int all = min(few + wides, x.most);
+  if (threadIdx.x == 0) *x.count = all;
+  for (int k = threadIdx.x; k < all; k += kPlan) x.piece[k] = piece_at<kPlan>(x, s, wides, k);
+}
+
+// The pieces that this work-group is to do, in todo[0 .. count - 1], the key-value head
+// of each in pad[0]; returns the count.  The (piece, head)s are dealt to the groups in turn,
+// there and back, so that a group plans once and does a few, and the last ones
+// go to the groups that began with the lightest.
+constexpr int kTodo = 8;
+
+__device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem) {
+  const uint32_t kv = x.c.kv_heads;
+  int few = 0, wides = 0;
+  if (x.mode == kOwnPlan) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, few, wides);
+  const int64_t all = (int64_t)(x.mode == kOwnPlan ? min(few + wides, x.most) : x.mode == kPlanned ? *x.count : x.most) * kv;
+  const int64_t f = (int64_t)threadIdx.x * gridDim.x + (threadIdx.x % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  if (threadIdx.x < kTodo && f < all) {
+    const int k = (int)((uint32_t)f / kv);
+    Piece p;
+    if (x.mode == kOwnPlan) {
+      p = piece_at<256>(x, *(Plan<256>*)smem, wides, k);
+    } else if (x.mode == kPlanned) {
+      p = x.piece[k];
+    } else {                                        // kWhole: a sequence's rows against all its keys
+      const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, tiles = up_to(rows, x.tile);
+      p.first = (int)((uint32_t)k / (uint32_t)tiles);
+      p.seg_rows = rows;
+      p.row0 = (k - p.first * tiles) * x.tile;
+      p.rows = min(x.tile, rows - p.row0);
+      const int id = x.ids ? x.ids[p.first] : p.first;
+      p.k0 = 0;
+      p.k1 = known_len(x, id);
+      p.table = in_range(id, x.c.seqs) ? id : 0;
+      p.see = p.k1 - x.a.q_len + 1;
+      p.slot = -1;
+      p.wide = 0;
+    }
+    p.pad[0] = (int)((uint32_t)f - (uint32_t)k * kv);
+    todo[threadIdx.x] = p;
+  }
+  return __syncthreads_count(threadIdx.x < kTodo && f < all);
 }
 
 // ---------------------------------------------------------------------------
@@ -241,20 +362,6 @@ template <>
 struct VRow<96> { typedef uint32_t type __attribute__((ext_vector_type(3), aligned(4))); };
 template <>
 struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(16))); };
-
-struct Args {
-  Cache c;
-  Queries a;
-  float sc;                            // scale * log2(e)
-  const uint16_t *q, *kp, *vp;
-  const int32_t* tables;
-  const int32_t* count;
-  const Piece* piece;
-  float2* ml;
-  float* part;
-  uint16_t* o;
-  float* lse;
-};
 
 template <int D, int NT>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int kh, float* lds) {
@@ -295,6 +402,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   };
   u32x4_t kf[2][kC];
   VWords vr[8];
+  uint32_t poison = 0;                              // infinite or NaN values set aside
   auto half_at = [&](int i, int s, bool& ok) {      // element offset of half s of tile i
     const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + s);
     const int key = p.k0 + 32 * wave + 128 * i + 16 * s;
@@ -368,7 +476,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
         const float alpha = mn == m[u] ? 1.f : fast_exp2(m[u] - mn);
         l[u] *= alpha;
 #pragma unroll
-        for (int t = 0; t < kT; ++t) o[u][t] *= alpha;
+        for (int t = 0; t < kT; ++t)                 // in place, as in WaveRows::softmax
+#pragma unroll
+          for (int r = 0; r < 4; ++r) asm volatile("v_mul_f32 %0, %0, %1" : "+v"(o[u][t][r]) : "v"(alpha));
         m[u] = mn;
       }
       const float mb = m[u] == -INFINITY ? 0.f : m[u];
@@ -394,60 +504,33 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
         f[j] = __builtin_amdgcn_perm(vr[2 * j + 1][t >> 1], vr[2 * j][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
       return f;
     };
-    bool plain = true;
     if (masked) {
       // Slots that no row sees may hold anything: they count as 0 (0 * NaN is NaN).
-      // A value that some rows see and others don't must reach the former only.
-      uint32_t bad = 0;
+      // So do infinite and NaN values, which must not reach the rows that don't
+      // see them; the others get them at the end.
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool any = key0 + 16 * (e >> 2) + 4 * g + (e & 3) < p.k1 && (e >= 4 ? ok1 : ok0);
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
-          vr[e][w] = any ? vr[e][w] : 0;
-          bad |= (vr[e][w] & 0x7f80u) == 0x7f80u || (vr[e][w] & 0x7f800000u) == 0x7f800000u;
+          const uint32_t v = any ? vr[e][w] : 0;
+          const uint32_t bad = ((v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+          vr[e][w] = v & ~bad;
+          poison |= bad;
         }
       }
-      plain = !__builtin_amdgcn_ballot_w64(bad != 0);
     }
-    if (plain) {
 #pragma unroll
-      for (int t = 0; t < kT; ++t) {
-        const u32x4_t f = frag(t);
+    for (int t = 0; t < kT; ++t) {
+      const u32x4_t f = frag(t);
 #pragma unroll
-        for (int u = 0; u < NT; ++u) o[u][t] = mfma16x16x32(f, pb[u], o[u][t]);
-      }
-    } else {
-      // Token by token of the queries: the keys its rows see, added to their columns.
-      for (int w = 0, last = p.k0; w < x.a.q_len; ++w) {
-        const int end = min(p.see + w, p.k1);
-        if (end <= last) continue;
-        last = end;
-        uint32_t keep[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = key0 + 16 * (j >> 1) + 4 * g + 2 * (j & 1);
-          keep[j] = (key < end ? 0xffffu : 0u) | (key + 1 < end ? 0xffff0000u : 0u);
-        }
-#pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          u32x4_t f = frag(t);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] &= keep[j];
-#pragma unroll
-          for (int u = 0; u < NT; ++u) {
-            const f32x4_t y = mfma16x16x32(f, pb[u], f32x4_t{});
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[u][t][r] += see[u] == end ? y[r] : 0.f;
-          }
-        }
-      }
+      for (int u = 0; u < NT; ++u) o[u][t] = mfma16x16x32(f, pb[u], o[u][t]);
     }
     if (more) load_v(i + 1);
   }
   // Join the waves.
   float* mls = lds + 4 * kRows * kStride;
-  __syncthreads();
+  const bool poisoned = __syncthreads_or(poison != 0);
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     const float lt = quad_sum(l[u]);
@@ -475,6 +558,17 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
       lt += f * mls[2 * (w * kRows + r) + 1];
       sum += f * *(const f32x4_t*)(lds + (w * kRows + r) * kStride + d);
     }
+    if (poisoned) {                                 // infinite and NaN values of the keys that row r sees
+      const int end = min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1);
+      for (int key = p.k0; key < end; ++key) {
+        const int id = table[key / page];
+        if (!in_range(id, x.c.pages)) continue;
+        const uint16_t* v = x.vp + (((size_t)id * x.c.kv_heads + kh) * page + (key & (page - 1))) * D + d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((v[i] & 0x7f80) == 0x7f80) sum[i] += __builtin_bit_cast(float, (uint32_t)v[i] << 16);
+      }
+    }
     if (p.slot >= 0) {
       const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + r;
       *(f32x4_t*)(x.part + at * D + d) = sum;
@@ -492,10 +586,11 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
 // A piece of up to 128 rows, all of which see all its keys (whole tiles of
 // 64): the software pipeline of the dense kernel (WaveRows::step), four waves
 // of 32 rows over rings of two K and two V tiles in LDS.  A wave copies 16
-// consecutive keys of a tile, which lie in one page.
+// consecutive keys of a tile, which lie in one page.  False, with nothing
+// done, if some page id of the piece names no page.
 // ---------------------------------------------------------------------------
 template <int D>
-__device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, int kh, char* smem) {
+__device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh, char* smem) {
   using G = Geo<D>;
   constexpr int kT = Swizzle<D>::kTile, kC = TileCopy<D, 4>::kPer;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -517,6 +612,9 @@ __device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, int kh
 #pragma unroll
     for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
   }
+  bool bad = false;
+  for (int j = p.k0 / page + tid; j <= (p.k1 - 1) / page; j += 256) bad |= !in_range(table[j], x.c.pages);
+  if (__syncthreads_or(bad)) return false;
   TileCopy<D, 4> cp;
   ReadAddr<D> ra;
   cp.init(wave, lane);
@@ -597,11 +695,11 @@ __device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, int kh
     s0[1] = s1[1];
     ++it;
   }
-  if (!active) return;
+  if (!active) return true;
   w.template step<2, false, true, 0>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
   const float lt = pair_sum(w.l);
   const int q = 32 * wave + (lane & 31), h = lane >> 5;
-  if (q >= p.rows) return;
+  if (q >= p.rows) return true;
   const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + q;
 #pragma unroll
   for (int t = 0; t < G::kDTiles; ++t)
@@ -610,35 +708,37 @@ __device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, int kh
       *(f32x4_t*)(x.part + at * D + 32 * t + 8 * j + 4 * h) =
           f32x4_t{w.o[t][4 * j], w.o[t][4 * j + 1], w.o[t][4 * j + 2], w.o[t][4 * j + 3]};
   if (h == 0) x.ml[at] = float2{w.m, lt};
+  return true;
 }
 
 template <int D, int NT, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 piece_kernel(Args x) {
-  constexpr int kJoin = 4 * 16 * NT * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
+  constexpr int kJoin = 4 * 16 * (kShared ? 2 : NT) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
-  const int i = blockIdx.x / x.c.kv_heads, kh = blockIdx.x % x.c.kv_heads;
-  if (i >= *x.count) return;
-  const Piece p = x.piece[i];
-  if constexpr (kShared) {
-    bool whole = false;
-    if (p.wide) {                                   // every page id of the piece names a page
-      const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
-      bool bad = false;
-      for (int j = p.k0 / x.c.page + threadIdx.x; j <= (p.k1 - 1) / x.c.page; j += 256) bad |= !in_range(table[j], x.c.pages);
-      whole = !__syncthreads_or(bad);
-      if (whole) tile_piece<D>(x, p, kh, smem);
+  static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
+  __shared__ Piece todo[kTodo];
+  const int count = my_pieces(x, todo, smem);
+  for (int i = 0; i < count; ++i) {
+    Piece p = todo[i];
+    int32_t* w = (int32_t*)&p;                     // the same in every lane
+#pragma unroll
+    for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
+    const int kh = p.pad[0];
+    if (i > 0) __syncthreads();                     // the piece before has left the LDS
+    if constexpr (kShared) {
+      if (p.wide && tile_piece<D>(x, p, kh, smem)) continue;
+      // A few rows, or, where a page is missing, many a few at a time.
+      Piece s = p;
+      for (int r = 0; r < p.rows; r += 32) {
+        s.row0 = p.row0 + r;
+        s.rows = min(32, p.rows - r);
+        if (NT == 2 || s.rows > 16) stream_piece<D, 2>(x, s, kh, (float*)smem);
+        else stream_piece<D, 1>(x, s, kh, (float*)smem);
+      }
+    } else {
+      stream_piece<D, NT>(x, p, kh, (float*)smem);
     }
-    if (whole) return;
-    // A few rows, or, where a page is missing, many a few at a time.
-    Piece s = p;
-    for (int r = 0; r < p.rows; r += 16 * NT) {
-      s.row0 = p.row0 + r;
-      s.rows = min(16 * NT, p.rows - r);
-      stream_piece<D, NT>(x, s, kh, (float*)smem);
-    }
-  } else {
-    stream_piece<D, NT>(x, p, kh, (float*)smem);
   }
 }
 
@@ -647,48 +747,50 @@ piece_kernel(Args x) {
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ void __launch_bounds__(256)
-join_kernel(Args x, const Joint* __restrict__ joint, int64_t all) {
+join_kernel(Args x, int64_t all) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = (int64_t)blockIdx.x * 4 + wave;
   if (row >= all) return;
   const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, kv = x.c.kv_heads;
   const int r = (int)(row % rows), kh = (int)(row / rows % kv), b = (int)(row / rows / kv);
-  const Joint j = joint[b];
+  const Joint j = x.joint[b];
   if (j.done) return;
   const int pieces = j.pre_pieces + j.own_pieces;
   auto slot = [&](int i) {
     return i < j.pre_pieces ? (size_t)j.pre_slot + ((size_t)i * kv + kh) * j.pre_rows + j.pre_row0 + r
                             : (size_t)j.own_slot + ((size_t)(i - j.pre_pieces) * kv + kh) * rows + r;
   };
-  float m = -INFINITY;
-  for (int i = lane; i < pieces; i += 64) m = fmaxf(m, x.ml[slot(i)].x);
+  float2 y[8];                                      // the results of eight pieces in flight
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      y[w] = float2{0.f, 0.f};
+      if (i0 + w < pieces && lane < D / 2) y[w] = *(const float2*)(x.part + slot(i0 + w) * D + 2 * lane);
+    }
+  };
+  load(0);
+  float2 ml = lane < pieces ? x.ml[slot(lane)] : float2{-INFINITY, 0.f};
+  float m = ml.x;
+  for (int i = lane + 64; i < pieces; i += 64) m = fmaxf(m, x.ml[slot(i)].x);
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor(m, w, 64));
   const float mb = m == -INFINITY ? 0.f : m;
   float l = 0.f, o0 = 0.f, o1 = 0.f;
   for (int i0 = 0; i0 < pieces; i0 += 64) {
-    float f = 0.f;
-    if (i0 + lane < pieces) {
-      const float2 y = x.ml[slot(i0 + lane)];
-      f = fast_exp2(y.x - mb);
-      l += f * y.y;
-    }
+    if (i0 > 0) ml = i0 + lane < pieces ? x.ml[slot(i0 + lane)] : float2{-INFINITY, 0.f};
+    const float f = fast_exp2(ml.x - mb);
+    l += f * ml.y;
     const int end = min(64, pieces - i0);
-    for (int i = 0; i < end; i += 8) {               // eight loads in flight
-      float2 y[8];
+    for (int i = 0; i < end; i += 8) {
 #pragma unroll
       for (int w = 0; w < 8; ++w) {
-        y[w] = float2{0.f, 0.f};
-        if (i + w < end && lane < D / 2) y[w] = *(const float2*)(x.part + slot(i0 + i + w) * D + 2 * lane);
-      }
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        const float fi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (i + w) & 63));
+        const float fi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i + w));
         if (i + w < end) {
           o0 += fi * y[w].x;
           o1 += fi * y[w].y;
         }
       }
+      load(i0 + i + 8);
     }
   }
 #pragma unroll
@@ -699,14 +801,22 @@ join_kernel(Args x, const Joint* __restrict__ joint, int64_t all) {
 }
 
 template <int D, int NT>
-hipError_t launch(const Args& x, const Joint* joint, bool shared, int64_t pieces, hipStream_t st) {
-  const unsigned grid = (unsigned)(pieces * x.c.kv_heads);
-  if (shared) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
-  else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+hipError_t launch(const Args& x, hipStream_t st) {
   const int64_t rows = (int64_t)x.a.batch * x.a.heads * x.a.q_len;
-  join_kernel<D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(x, joint, rows);
+  if (x.mode == kPlanned) {
+    plan_kernel<<<1, kPlan, 0, st>>>(x);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  // As many groups as the chip holds at once (registers allow a CU so many),
+  // or as do all the pieces kTodo at a time.
+  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * (x.shared != nullptr ? 2 : D == 64 && NT == 1 ? 4 : NT == 1 || D == 64 ? 3 : 2);
+  const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
+  if (x.shared != nullptr) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
+  else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || x.mode == kWhole) return e;
+  join_kernel<D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(x, rows);
   return hipGetLastError();
 }
 
@@ -719,20 +829,25 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
                          hipStream_t st) {
   Space s;
   space_bytes(c, a, ws, &s);
-  const Limits l = limits(c, a);
-  const int tile = row_tile(c, a);
-  plan_kernel<<<1, kPlan, 0, st>>>(c, a, tile, l.pieces, ids, lens, shared, s.count, s.joint, s.piece);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const Args x{c, a, a.scale * kLog2e, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, tables, s.count, s.piece, s.ml,
-               s.part, (uint16_t*)o, lse};
-  switch (c.head_dim + tile) {
-    case 64 + 16: return launch<64, 1>(x, s.joint, shared != nullptr, l.pieces, st);
-    case 96 + 16: return launch<96, 1>(x, s.joint, shared != nullptr, l.pieces, st);
-    case 128 + 16: return launch<128, 1>(x, s.joint, shared != nullptr, l.pieces, st);
-    case 64 + 32: return launch<64, 2>(x, s.joint, shared != nullptr, l.pieces, st);
-    case 96 + 32: return launch<96, 2>(x, s.joint, shared != nullptr, l.pieces, st);
-    default: return launch<128, 2>(x, s.joint, shared != nullptr, l.pieces, st);
+  Args x;
+  x.c = c;
+  x.a = a;
+  x.sc = a.scale * kLog2e;
+  x.tile = row_tile(c, a);
+  x.mode = shared == nullptr && (int64_t)c.max_pages * c.page <= kWholeKeys ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
+  const int rows = a.heads / c.kv_heads * a.q_len;
+  x.most = x.mode == kWhole ? a.batch * ((rows + x.tile - 1) / x.tile) : (int)limits(c, a).pieces;
+  x.q = (const uint16_t*)q, x.kp = (const uint16_t*)kp, x.vp = (const uint16_t*)vp;
+  x.tables = tables, x.lens = lens, x.ids = ids, x.shared = shared;
+  x.count = s.count, x.joint = s.joint, x.piece = s.piece, x.ml = s.ml, x.part = s.part;
+  x.o = (uint16_t*)o, x.lse = lse;
+  switch (c.head_dim + x.tile) {
+    case 64 + 16: return launch<64, 1>(x, st);
+    case 96 + 16: return launch<96, 1>(x, st);
+    case 128 + 16: return launch<128, 1>(x, st);
+    case 64 + 32: return launch<64, 2>(x, st);
+    case 96 + 32: return launch<96, 2>(x, st);
+    default: return launch<128, 2>(x, st);
   }
 }
 

@@ -83,6 +83,7 @@ wise_status check_queries(const wise_cache* c, const wise_queries* a, wise::Cach
   if (a->batch <= 0 || a->heads <= 0 || a->q_len <= 0 || a->heads % c->kv_heads != 0) return WISE_ERR_SHAPE;
   if (a->batch > wise::kMaxEntries || (int64_t)(a->heads / c->kv_heads) * a->q_len > wise::kMaxQueryRows)
     return WISE_ERR_UNSUPPORTED;
+  if ((int64_t)a->batch * a->heads > kI32Max / ((int64_t)a->q_len * c->head_dim)) return WISE_ERR_SHAPE;
   if (isnan(a->scale) || isinf(a->scale)) return WISE_ERR_RANGE;
   *out = wise::Queries{a->batch, a->heads, a->q_len, a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)};
   return WISE_OK;
