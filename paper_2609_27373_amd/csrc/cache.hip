@@ -13,6 +13,8 @@
 namespace wise {
 namespace {
 
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ int clamp_len(int len, const Cache& c) {
   const int cap = c.max_pages * c.page;
   return len < 0 ? 0 : len > cap ? cap : len;
@@ -117,15 +119,21 @@ struct ReserveCopy {
 __global__ void __launch_bounds__(kPlan)
 reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32_t* __restrict__ counts, int32_t* tables,
                     int32_t* lens, int32_t* refs, int32_t* granted, int32_t* list, ReserveCopy* copies) {
-  __shared__ int32_t id_[kPlan], begin_[kPlan], row_[kPlan], first_[kPlan];
+  __shared__ __attribute__((aligned(16))) int32_t id_[kPlan];
+  __shared__ int32_t begin_[kPlan], row_[kPlan], first_[kPlan];
   __shared__ int64_t waves[kPlanWaves];
   const int i = threadIdx.x;
   const int s = i < n ? ids[i] : -1, count = i < n ? counts[i] : 0;
   id_[i] = s;
   __syncthreads();
-  bool again = false;
-#pragma unroll 8
-  for (int j = 0; j < n; ++j) again |= j < i && id_[j] == s;
+  bool again = false;                  // by the waves that have entries, against those before them
+  const int before = i < n ? (i | 63) + 1 : 0;
+#pragma unroll 4
+  for (int j = 0; j < before; j += 4) {
+    const i32x4_t y = *(const i32x4_t*)(id_ + j);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) again |= j + u < i && y[u] == s;
+  }
   bool ok = in_range(s, c.seqs) && count > 0 && !again;
   int len = 0, begin = 0, last = -1;
   int64_t need = 0;
@@ -173,26 +181,53 @@ reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32
   }
 }
 
-// Copies rows * d bf16 of every plane and head of an entry's last page.
+// Copies rows * d bf16 of every plane and head of an entry's last page: kCopyHeads
+// of them a work-group, as many side by side as its threads reach, four passes in flight.
+constexpr int kCopyHeads = 16;
+
 __global__ void __launch_bounds__(256)
 reserve_copy_kernel(Cache c, const ReserveCopy* __restrict__ copies, uint16_t* pool) {
   const ReserveCopy r = copies[blockIdx.x];
   if (r.rows == 0) return;
-  const size_t head = (size_t)c.page * c.head_dim, page = head * c.kv_heads;
-  const int chunks = r.rows * c.head_dim / 8;
-  const int64_t heads = (int64_t)c.planes * c.kv_heads;
-  for (int64_t x = blockIdx.y; x < heads; x += gridDim.y) {
-    const int64_t plane = x / c.kv_heads, h = x % c.kv_heads;
-    uint16_t* base = pool + plane * c.pages * page + h * head;
-    const u32x4_t* from = (const u32x4_t*)(base + (size_t)r.src * page);
-    u32x4_t* to = (u32x4_t*)(base + (size_t)r.dst * page);
-    for (int j = threadIdx.x; j < chunks; j += blockDim.x) to[j] = from[j];
+  const size_t head = (size_t)c.page * c.head_dim / 8, page = head * c.kv_heads;   // 16-byte chunks
+  const int chunks = r.rows * c.head_dim / 8, per = chunks < 256 ? 256 / chunks : 1;
+  const int mine = chunks < 256 ? threadIdx.x / chunks : 0;
+  if (mine >= per) return;
+  const uint32_t x0 = blockIdx.y * kCopyHeads, all = (uint32_t)(c.planes * c.kv_heads), x1 = min(x0 + kCopyHeads, all);
+  for (int ch = threadIdx.x - mine * chunks; ch < chunks; ch += 256) {
+    for (uint32_t x = x0 + mine; x < x1; x += 4 * per) {
+      u32x4_t w[4];
+      u32x4_t* to[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t y = x + u * per, plane = y / (uint32_t)c.kv_heads, h = y - plane * c.kv_heads;
+        if (y < x1) {
+          u32x4_t* base = (u32x4_t*)pool + (size_t)plane * c.pages * page + h * head + ch;
+          to[u] = base + (size_t)r.dst * page;
+          w[u] = base[(size_t)r.src * page];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (x + u * per < x1) *to[u] = w[u];
+    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// Append: a 16-byte chunk of a token row a thread, K and V.
+// Append.  A few tokens an entry: a 16-byte chunk of a token row a thread, K and
+// V.  Many: a work-group takes kAppendTile tokens of one entry and head, whose
+// sequence and length are then scalars, a few chunks a thread in flight.
 // ---------------------------------------------------------------------------
+constexpr int kAppendTile = 64;
+
+// Element offset in a plane of position pos of sequence s, head h; -1: nowhere.
+__device__ __forceinline__ int64_t slot_of(const Cache& c, const int32_t* tables, int s, int64_t pos, int h) {
+  if (pos < 0 || pos >= (int64_t)c.max_pages * c.page) return -1;
+  const int p = tables[(size_t)s * c.max_pages + (uint32_t)pos / (uint32_t)c.page];
+  return in_range(p, c.pages) ? (((int64_t)p * c.kv_heads + h) * c.page + (pos & (c.page - 1))) * c.head_dim : -1;
+}
+
 __global__ void __launch_bounds__(256)
 append_kernel(Cache c, int rows, int tokens, const int32_t* __restrict__ ids, const int32_t* __restrict__ counts,
               const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const int32_t* __restrict__ tables,
@@ -203,17 +238,50 @@ append_kernel(Cache c, int rows, int tokens, const int32_t* __restrict__ ids, co
   if (mine >= per || at >= rows) return;
   const uint32_t row = (uint32_t)at, t = row % (uint32_t)tokens, eh = row / (uint32_t)tokens;
   const uint32_t h = eh % (uint32_t)c.kv_heads, e = eh / (uint32_t)c.kv_heads;
+  const size_t from = (size_t)row * c.head_dim + 8 * ch;
   const int s = ids[e];
   const int count = min(counts[e], tokens);
   if (!in_range(s, c.seqs) || (int)t >= count) return;
-  const int64_t pos = (int64_t)lens[s] - count + (int)t;
-  if (pos < 0 || pos >= (int64_t)c.max_pages * c.page) return;
-  const int p = tables[(size_t)s * c.max_pages + pos / c.page];
-  if (!in_range(p, c.pages)) return;
-  const size_t to = (((size_t)p * c.kv_heads + h) * c.page + pos % c.page) * c.head_dim + 8 * ch;
-  const size_t from = (size_t)row * c.head_dim + 8 * ch;
-  *(u32x4_t*)(kp + to) = *(const u32x4_t*)(k + from);
-  *(u32x4_t*)(vp + to) = *(const u32x4_t*)(v + from);
+  const u32x4_t kw = *(const u32x4_t*)(k + from), vw = *(const u32x4_t*)(v + from);
+  const int64_t to = slot_of(c, tables, s, (int64_t)lens[s] - count + (int)t, h);
+  if (to < 0) return;
+  *(u32x4_t*)(kp + to + 8 * ch) = kw;
+  *(u32x4_t*)(vp + to + 8 * ch) = vw;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256)
+append_tile_kernel(Cache c, int tokens, int tiles, const int32_t* __restrict__ ids, const int32_t* __restrict__ counts,
+                   const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const int32_t* __restrict__ tables,
+                   const int32_t* __restrict__ lens, uint16_t* kp, uint16_t* vp) {
+  constexpr int kChunks = D / 8, kPer = kAppendTile * kChunks / 256;
+  const uint32_t tile = blockIdx.x % (uint32_t)tiles, eh = blockIdx.x / (uint32_t)tiles;
+  const uint32_t h = eh % (uint32_t)c.kv_heads, e = eh / (uint32_t)c.kv_heads;
+  const int s = ids[e], t0 = tile * kAppendTile;
+  const int count = min(counts[e], tokens);
+  if (!in_range(s, c.seqs) || t0 >= count) return;
+  const int64_t first = (int64_t)lens[s] - count;
+  const size_t from = (size_t)eh * tokens * D;
+  u32x4_t kw[kPer], vw[kPer];
+  int64_t to[kPer];
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int x = threadIdx.x + 256 * u, t = t0 + x / kChunks, ch = x % kChunks;
+    to[u] = -1;
+    if (t < count) {
+      kw[u] = *(const u32x4_t*)(k + from + (size_t)t * D + 8 * ch);
+      vw[u] = *(const u32x4_t*)(v + from + (size_t)t * D + 8 * ch);
+      to[u] = slot_of(c, tables, s, first + t, h);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int ch = (threadIdx.x + 256 * u) % kChunks;
+    if (to[u] >= 0) {
+      *(u32x4_t*)(kp + to[u] + 8 * ch) = kw[u];
+      *(u32x4_t*)(vp + to[u] + 8 * ch) = vw[u];
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -328,19 +396,26 @@ hipError_t launch_cache_reserve(const Cache& c, int n, const int32_t* ids, const
   reserve_plan_kernel<<<1, kPlan, 0, st>>>(c, n, ids, counts, tables, lens, refs, granted, w.src, w.copies);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t heads = (int64_t)c.planes * c.kv_heads;
-  const dim3 grid(n, (unsigned)(heads < 1024 ? heads : 1024));
+  const dim3 grid(n, (unsigned)((c.planes * c.kv_heads + kCopyHeads - 1) / kCopyHeads));
   reserve_copy_kernel<<<grid, 256, 0, st>>>(c, w.copies, (uint16_t*)pool);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_append(const Cache& c, int n, int tokens, const int32_t* ids, const int32_t* counts, const void* k,
                                const void* v, const int32_t* tables, const int32_t* lens, void* kp, void* vp, hipStream_t st) {
-  const int rows = n * c.kv_heads * tokens, per = 256 / (c.head_dim / 8);
-  append_kernel<<<(unsigned)(((int64_t)rows + per - 1) / per), 256, 0, st>>>(c, rows, tokens, ids, counts, (const uint16_t*)k,
-                                                                             (const uint16_t*)v, tables, lens, (uint16_t*)kp,
-                                                                             (uint16_t*)vp);
-  return hipGetLastError();
+  const uint16_t *kk = (const uint16_t*)k, *vv = (const uint16_t*)v;
+  uint16_t *ko = (uint16_t*)kp, *vo = (uint16_t*)vp;
+  if (tokens < kAppendTile) {
+    const int rows = n * c.kv_heads * tokens, per = 256 / (c.head_dim / 8);
+    append_kernel<<<(unsigned)(((int64_t)rows + per - 1) / per), 256, 0, st>>>(c, rows, tokens, ids, counts, kk, vv, tables, lens, ko, vo);
+    return hipGetLastError();
+  }
+  const int tiles = (tokens + kAppendTile - 1) / kAppendTile;
+  const auto run = [&](auto kernel) {
+    kernel<<<(unsigned)(n * c.kv_heads * tiles), 256, 0, st>>>(c, tokens, tiles, ids, counts, kk, vv, tables, lens, ko, vo);
+    return hipGetLastError();
+  };
+  return c.head_dim == 64 ? run(append_tile_kernel<64>) : c.head_dim == 96 ? run(append_tile_kernel<96>) : run(append_tile_kernel<128>);
 }
 
 hipError_t launch_cache_compact(const Cache& c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,

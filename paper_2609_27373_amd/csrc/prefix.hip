@@ -55,6 +55,12 @@ struct Joint {
 #define WK 768
 #endif
 constexpr int kGroups = GR, kFewKeys = FK;
+#ifndef HOLD
+#define HOLD (x.shared != nullptr ? 2 : D == 64 && NT == 1 ? 3 : 2)
+#endif
+#ifndef AHEAD
+#define AHEAD (D * NT <= 128)
+#endif
 #ifndef MK
 #define MK 512
 #endif
@@ -123,7 +129,9 @@ struct Args {
   Cache c;
   Queries a;
   float sc;                            // scale * log2(e)
-  int tile;                            // rows of a piece of few rows
+  int rows;                            // query rows of a sequence per key-value head
+  int tile, tiles;                     // rows of a piece of few rows, such pieces of a sequence's rows
+  int page_bits;
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
   const uint16_t *q, *kp, *vp;
@@ -168,13 +176,24 @@ __device__ __forceinline__ int known_len(const Args& x, int id) {
 
 // Runs and pieces of all sequences: few and wides are the numbers of pieces of
 // either kind per key-value head.  Writes x.joint if `write`.
+// The planning threads are together: one wave needs no barrier for it.
+template <int kN>
+__device__ __forceinline__ void plan_sync() {
+  if constexpr (kN > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 template <int kN>
 __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int& wides) {
-  const int b = threadIdx.x, lane = b & 63, wave = b >> 6;
+  const int b = threadIdx.x, lane = b & 63, wave = kN > 64 ? b >> 6 : 0;
   const Cache& c = x.c;
   const Queries& a = x.a;
   const bool live = b < a.batch;
-  const int rows = a.heads / c.kv_heads * a.q_len, tile = x.tile;
+  const int rows = x.rows;
   const int id = !live ? -1 : x.ids ? x.ids[b] : b;
   const int sh = live && b > 0 && x.shared ? x.shared[b] : 0;
   const int len = known_len(x, id), see = len - a.q_len + 1;
@@ -182,23 +201,23 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   if (x.shared != nullptr) {
     // Runs: a sequence belongs to the last start at or before it.
     start = wave_scan_max(sh <= 0 ? b : 0);
-    if (lane == 63) s.wave_start[wave] = start;
+    if (kN > 64 && lane == 63) s.wave_start[wave] = start;
     s.members[b] = 0;
     s.pre_keys[b] = s.see[b] = 0x7fffffff;
-    __syncthreads();
+    plan_sync<kN>();
     for (int w = 0; w < wave; ++w) start = max(start, s.wave_start[w]);
     if (live) {
       atomicAdd(&s.members[start], 1);
       atomicMin(&s.see[start], see);
       if (b != start) atomicMin(&s.pre_keys[start], sh);
     }
-    __syncthreads();
+    plan_sync<kN>();
     // What the run reads once: whole pages that every query sees, in whole
     // tiles of 64 keys (so that no piece of them needs a mask).
     n = s.members[start];
-    if (n > 1) pre = (min(s.pre_keys[start], max(s.see[start], 0) / c.page) * c.page) & ~63;
+    if (n > 1) pre = (min(s.pre_keys[start], max(s.see[start], 0) >> x.page_bits) << x.page_bits) & ~63;
   }
-  const int own = len - pre, own_tiles = up_to(rows, tile);
+  const int own = len - pre, own_tiles = x.tiles;
   const bool leads = live && b == start && pre > 0;
   const int pre_rows = leads ? n * rows : 0;
   const bool wide = pre_rows > kWideRows;
@@ -206,15 +225,17 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   int64_t k0 = (int64_t)own_tiles * own + (wide ? 0 : (int64_t)pre_tiles * pre), k1 = wide ? (int64_t)pre_tiles * pre : 0;
   k0 = wave_total(k0);
   k1 = x.shared != nullptr ? wave_total(k1) : 0;
-  if (lane == 0) {
-    s.wave_keys[wave][0] = k0;
-    s.wave_keys[wave][1] = k1;
-  }
-  __syncthreads();
-  k0 = k1 = 0;
-  for (int w = 0; w < kN / 64; ++w) {
-    k0 += s.wave_keys[w][0];
-    k1 += s.wave_keys[w][1];
+  if constexpr (kN > 64) {
+    if (lane == 0) {
+      s.wave_keys[wave][0] = k0;
+      s.wave_keys[wave][1] = k1;
+    }
+    __syncthreads();
+    k0 = k1 = 0;
+    for (int w = 0; w < kN / 64; ++w) {
+      k0 += s.wave_keys[w][0];
+      k1 += s.wave_keys[w][1];
+    }
   }
   auto even = [&](int64_t sum, int groups, int least) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
@@ -228,16 +249,21 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   const int mine[3] = {own_n * own_tiles + (wide ? 0 : pre_n * pre_tiles), wide ? pre_n * pre_tiles : 0,
                        (done ? 0 : own_n * c.kv_heads * rows) + pre_n * c.kv_heads * pre_rows};
   int sum[3] = {wave_scan_add(mine[0]), x.shared != nullptr ? wave_scan_add(mine[1]) : 0, wave_scan_add(mine[2])};
-  if (lane == 63)
+  if constexpr (kN > 64) {
+    if (lane == 63)
 #pragma unroll
-    for (int i = 0; i < 3; ++i) s.wave_sum[wave][i] = sum[i];
-  __syncthreads();
-  few = wides = 0;
-  for (int w = 0; w < kN / 64; ++w) {
+      for (int i = 0; i < 3; ++i) s.wave_sum[wave][i] = sum[i];
+    __syncthreads();
+    few = wides = 0;
+    for (int w = 0; w < kN / 64; ++w) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) sum[i] += w < wave ? s.wave_sum[w][i] : 0;
-    few += s.wave_sum[w][0];
-    wides += s.wave_sum[w][1];
+      for (int i = 0; i < 3; ++i) sum[i] += w < wave ? s.wave_sum[w][i] : 0;
+      few += s.wave_sum[w][0];
+      wides += s.wave_sum[w][1];
+    }
+  } else {
+    few = __builtin_amdgcn_readlane(sum[0], 63);
+    wides = __builtin_amdgcn_readlane(sum[1], 63);
   }
   s.first[b] = sum[0] - mine[0];
   s.wide_first[b] = sum[1] - mine[1];
@@ -250,7 +276,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   s.pre_len[b] = pre_l;
   if (x.shared == nullptr) s.members[b] = 1;
   s.pre_keys[b] = pre;
-  __syncthreads();
+  plan_sync<kN>();
   if (write && live)
     x.joint[b] = Joint{s.pre_slot[start], pre > 0 ? s.pre_pieces[start] : 0, n * rows, (b - start) * rows, s.own_slot[b], own_n, done, 0};
 }
@@ -258,7 +284,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
 // Piece k of a plan: those of many rows first.
 template <int kN>
 __device__ Piece piece_at(const Args& x, const Plan<kN>& s, int wides, int k) {
-  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, kv = x.c.kv_heads;
+  const int rows = x.rows, kv = x.c.kv_heads;
   Piece p;
   p.wide = k < wides;
   const int32_t* first = p.wide ? s.wide_first : s.first;
@@ -281,9 +307,9 @@ __device__ Piece piece_at(const Args& x, const Plan<kN>& s, int wides, int k) {
   } else {
     j -= pre_all;
     tile = x.tile;
-    const int own_tiles = up_to(rows, tile), i = (uint32_t)j / (uint32_t)own_tiles;
+    const int i = x.tiles == 1 ? j : (uint32_t)j / (uint32_t)x.tiles;
     p.seg_rows = rows;
-    p.row0 = (j - i * own_tiles) * tile;
+    p.row0 = (j - i * x.tiles) * tile;
     p.k0 = s.pre_keys[e] + i * s.own_len[e];
     p.k1 = min(p.k0 + s.own_len[e], s.len[e]);
     p.see = s.len[e] - x.a.q_len + 1;
@@ -313,22 +339,25 @@ constexpr int kTodo = 8;
 __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem) {
   const uint32_t kv = x.c.kv_heads;
   int few = 0, wides = 0;
-  if (x.mode == kOwnPlan) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, few, wides);
+  const bool one_wave = x.a.batch <= 64;
+  if (x.mode == kOwnPlan) {
+    if (!one_wave) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, few, wides);
+    else if (threadIdx.x < 64) make_plan<64>(x, *(Plan<64>*)smem, blockIdx.x == 0, few, wides);
+  }
   const int64_t all = (int64_t)(x.mode == kOwnPlan ? min(few + wides, x.most) : x.mode == kPlanned ? *x.count : x.most) * kv;
   const int64_t f = (int64_t)threadIdx.x * gridDim.x + (threadIdx.x % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
   if (threadIdx.x < kTodo && f < all) {
     const int k = (int)((uint32_t)f / kv);
     Piece p;
     if (x.mode == kOwnPlan) {
-      p = piece_at<256>(x, *(Plan<256>*)smem, wides, k);
+      p = one_wave ? piece_at<64>(x, *(Plan<64>*)smem, wides, k) : piece_at<256>(x, *(Plan<256>*)smem, wides, k);
     } else if (x.mode == kPlanned) {
       p = x.piece[k];
     } else {                                        // kWhole: a sequence's rows against all its keys
-      const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, tiles = up_to(rows, x.tile);
-      p.first = (int)((uint32_t)k / (uint32_t)tiles);
-      p.seg_rows = rows;
-      p.row0 = (k - p.first * tiles) * x.tile;
-      p.rows = min(x.tile, rows - p.row0);
+      p.first = x.tiles == 1 ? k : (int)((uint32_t)k / (uint32_t)x.tiles);
+      p.seg_rows = x.rows;
+      p.row0 = (k - p.first * x.tiles) * x.tile;
+      p.rows = min(x.tile, x.rows - p.row0);
       const int id = x.ids ? x.ids[p.first] : p.first;
       p.k0 = 0;
       p.k1 = known_len(x, id);
@@ -366,10 +395,11 @@ struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), alig
 template <int D, int NT>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int kh, float* lds) {
   constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT;
+  constexpr bool kAhead = AHEAD;
   typedef typename VRow<D>::type VWords;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
-  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, page = x.c.page;
+  const int rows = x.rows, page = x.c.page;
   const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
   u32x4_t qf[NT][kC];
   int see[NT];
@@ -397,11 +427,11 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   int ids = -1;
   auto load_ids = [&](int i0) {
     const int key = p.k0 + 32 * wave + 128 * (i0 + (lane >> 1)) + 16 * (lane & 1);
-    ids = key < p.k1 ? table[key / page] : -1;
+    ids = key < p.k1 ? table[key >> x.page_bits] : -1;
     if (!in_range(ids, x.c.pages)) ids = -1;
   };
   u32x4_t kf[2][kC];
-  VWords vr[8];
+  VWords va[8], vb[8];
   uint32_t poison = 0;                              // infinite or NaN values set aside
   auto half_at = [&](int i, int s, bool& ok) {      // element offset of half s of tile i
     const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + s);
@@ -418,7 +448,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
       for (int e = 0; e < kC; ++e) kf[s][e] = *(const u32x4_t*)(base + n * D + 8 * g + 32 * e);
     }
   };
-  auto load_v = [&](int i) {
+  auto load_v = [&](int i, VWords (&vr)[8]) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       bool ok;
@@ -430,9 +460,10 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   if (tiles > 0) {
     load_ids(0);
     load_k(0);
-    load_v(0);
+    load_v(0, va);
   }
-  for (int i = 0; i < tiles; ++i) {
+  // Tile i, its V in vr; the next tile's K and V (into vn) are loaded meanwhile.
+  auto tile = [&](int i, VWords (&vr)[8], VWords (&vn)[8]) {
     const int key0 = p.k0 + 32 * wave + 128 * i;
     bool ok0, ok1;
     half_at(i, 0, ok0);
@@ -451,6 +482,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
     if (more) {
       if (((i + 1) & 31) == 0) load_ids(i + 1);
       load_k(i + 1);
+      if constexpr (kAhead) load_v(i + 1, vn);
     }
     if (masked) {
 #pragma unroll
@@ -526,7 +558,17 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
 #pragma unroll
       for (int u = 0; u < NT; ++u) o[u][t] = mfma16x16x32(f, pb[u], o[u][t]);
     }
-    if (more) load_v(i + 1);
+    if (!kAhead && more) load_v(i + 1, vn);
+  };
+  if constexpr (kAhead) {
+    int i = 0;
+    for (; i + 1 < tiles; i += 2) {
+      tile(i, va, vb);
+      tile(i + 1, vb, va);
+    }
+    if (i < tiles) tile(i, va, vb);
+  } else {
+    for (int i = 0; i < tiles; ++i) tile(i, va, va);
   }
   // Join the waves.
   float* mls = lds + 4 * kRows * kStride;
@@ -542,7 +584,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < kT; ++t) lds[r * kStride + kT * (4 * g + i) + t] = o[u][t][i];
+      for (int t = 0; t < kT; t += 2) *(f32x2_t*)(lds + r * kStride + kT * (4 * g + i) + t) = f32x2_t{o[u][t][i], o[u][t + 1][i]};
   }
   __syncthreads();
   for (int j = tid; j < p.rows * (D / 4); j += 256) {
@@ -561,7 +603,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
     if (poisoned) {                                 // infinite and NaN values of the keys that row r sees
       const int end = min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1);
       for (int key = p.k0; key < end; ++key) {
-        const int id = table[key / page];
+        const int id = table[key >> x.page_bits];
         if (!in_range(id, x.c.pages)) continue;
         const uint16_t* v = x.vp + (((size_t)id * x.c.kv_heads + kh) * page + (key & (page - 1))) * D + d;
 #pragma unroll
@@ -594,13 +636,13 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh
   using G = Geo<D>;
   constexpr int kT = Swizzle<D>::kTile, kC = TileCopy<D, 4>::kPer;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, page = x.c.page;
+  const int rows = x.rows, page = x.c.page;
   const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
   const int tiles = (p.k1 - p.k0) / kKeyTile;
   // Page ids of this wave's keys: lane i has the one of tile 64 u + i, of stretch u and the next one.
   auto load_ids = [&](int u) {
     const int key = p.k0 + (64 * u + lane) * kKeyTile + 16 * wave;
-    return key < p.k1 ? table[key / page] : 0;
+    return key < p.k1 ? table[key >> x.page_bits] : 0;
   };
   int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
   WaveRows<D> w;
@@ -613,7 +655,7 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh
     for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
   }
   bool bad = false;
-  for (int j = p.k0 / page + tid; j <= (p.k1 - 1) / page; j += 256) bad |= !in_range(table[j], x.c.pages);
+  for (int j = (p.k0 >> x.page_bits) + tid; j <= (p.k1 - 1) >> x.page_bits; j += 256) bad |= !in_range(table[j], x.c.pages);
   if (__syncthreads_or(bad)) return false;
   TileCopy<D, 4> cp;
   ReadAddr<D> ra;
@@ -751,7 +793,7 @@ join_kernel(Args x, int64_t all) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = (int64_t)blockIdx.x * 4 + wave;
   if (row >= all) return;
-  const int rows = x.a.heads / x.c.kv_heads * x.a.q_len, kv = x.c.kv_heads;
+  const int rows = x.rows, kv = x.c.kv_heads;
   const int r = (int)(row % rows), kh = (int)(row / rows % kv), b = (int)(row / rows / kv);
   const Joint j = x.joint[b];
   if (j.done) return;
@@ -810,7 +852,7 @@ hipError_t launch(const Args& x, hipStream_t st) {
   }
   // As many groups as the chip holds at once (registers allow a CU so many),
   // or as do all the pieces kTodo at a time.
-  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * (x.shared != nullptr ? 2 : D == 64 && NT == 1 ? 4 : NT == 1 || D == 64 ? 3 : 2);
+  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * HOLD;
   const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
   if (x.shared != nullptr) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
   else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
@@ -835,8 +877,10 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
   x.sc = a.scale * kLog2e;
   x.tile = row_tile(c, a);
   x.mode = shared == nullptr && (int64_t)c.max_pages * c.page <= kWholeKeys ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
-  const int rows = a.heads / c.kv_heads * a.q_len;
-  x.most = x.mode == kWhole ? a.batch * ((rows + x.tile - 1) / x.tile) : (int)limits(c, a).pieces;
+  x.rows = a.heads / c.kv_heads * a.q_len;
+  x.tiles = (x.rows + x.tile - 1) / x.tile;
+  x.page_bits = __builtin_ctz(c.page);
+  x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;
   x.q = (const uint16_t*)q, x.kp = (const uint16_t*)kp, x.vp = (const uint16_t*)vp;
   x.tables = tables, x.lens = lens, x.ids = ids, x.shared = shared;
   x.count = s.count, x.joint = s.joint, x.piece = s.piece, x.ml = s.ml, x.part = s.part;
