@@ -415,7 +415,7 @@ typedef struct {
   int32_t head_dim;  /* 64, 96 or 128                                        */
   int32_t planes;    /* planes of the pool: 2 x layers                       */
   int32_t seqs;      /* rows of tables and lens                              */
-  int32_t max_pages; /* columns of tables; max_pages * page < 2^31           */
+  int32_t max_pages; /* columns of tables; max_pages * page <= 2^30          */
 } wise_cache;
 
 /*

@@ -183,17 +183,18 @@ reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32
 
 // Copies rows * d bf16 of every plane and head of an entry's last page: kCopyHeads
 // of them a work-group, as many side by side as its threads reach, four passes in flight.
+// The stores, here and below, pass the L2 by: nothing reads them before other kernels do.
 constexpr int kCopyHeads = 16;
 
 __global__ void __launch_bounds__(256)
 reserve_copy_kernel(Cache c, const ReserveCopy* __restrict__ copies, uint16_t* pool) {
-  const ReserveCopy r = copies[blockIdx.x];
+  const ReserveCopy r = copies[blockIdx.y];
   if (r.rows == 0) return;
   const size_t head = (size_t)c.page * c.head_dim / 8, page = head * c.kv_heads;   // 16-byte chunks
   const int chunks = r.rows * c.head_dim / 8, per = chunks < 256 ? 256 / chunks : 1;
   const int mine = chunks < 256 ? threadIdx.x / chunks : 0;
   if (mine >= per) return;
-  const uint32_t x0 = blockIdx.y * kCopyHeads, all = (uint32_t)(c.planes * c.kv_heads), x1 = min(x0 + kCopyHeads, all);
+  const uint32_t x0 = blockIdx.x * kCopyHeads, all = (uint32_t)(c.planes * c.kv_heads), x1 = min(x0 + kCopyHeads, all);
   for (int ch = threadIdx.x - mine * chunks; ch < chunks; ch += 256) {
     for (uint32_t x = x0 + mine; x < x1; x += 4 * per) {
       u32x4_t w[4];
@@ -209,17 +210,18 @@ reserve_copy_kernel(Cache c, const ReserveCopy* __restrict__ copies, uint16_t* p
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (x + u * per < x1) *to[u] = w[u];
+        if (x + u * per < x1) __builtin_nontemporal_store(w[u], to[u]);
     }
   }
 }
 
 // ---------------------------------------------------------------------------
 // Append.  A few tokens an entry: a 16-byte chunk of a token row a thread, K and
-// V.  Many: a work-group takes kAppendTile tokens of one entry and head, whose
-// sequence and length are then scalars, a few chunks a thread in flight.
+// V.  Many: a work-group takes some of one entry and head, whose sequence and
+// length are then scalars, a few chunks a thread in flight.
 // ---------------------------------------------------------------------------
-constexpr int kAppendTile = 64;
+constexpr int kManyTokens = 64;
+constexpr int append_tile(int d) { return d == 96 ? 64 : 32; }   // tokens a work-group
 
 // Element offset in a plane of position pos of sequence s, head h; -1: nowhere.
 __device__ __forceinline__ int64_t slot_of(const Cache& c, const int32_t* tables, int s, int64_t pos, int h) {
@@ -254,10 +256,11 @@ __global__ void __launch_bounds__(256)
 append_tile_kernel(Cache c, int tokens, int tiles, const int32_t* __restrict__ ids, const int32_t* __restrict__ counts,
                    const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const int32_t* __restrict__ tables,
                    const int32_t* __restrict__ lens, uint16_t* kp, uint16_t* vp) {
-  constexpr int kChunks = D / 8, kPer = kAppendTile * kChunks / 256;
+  constexpr int kTile = append_tile(D), kChunks = D / 8, kPer = kTile * kChunks / 256;
+  static_assert(kTile * kChunks % 256 == 0, "whole chunks a thread");
   const uint32_t tile = blockIdx.x % (uint32_t)tiles, eh = blockIdx.x / (uint32_t)tiles;
   const uint32_t h = eh % (uint32_t)c.kv_heads, e = eh / (uint32_t)c.kv_heads;
-  const int s = ids[e], t0 = tile * kAppendTile;
+  const int s = ids[e], t0 = tile * kTile;
   const int count = min(counts[e], tokens);
   if (!in_range(s, c.seqs) || t0 >= count) return;
   const int64_t first = (int64_t)lens[s] - count;
@@ -269,8 +272,8 @@ append_tile_kernel(Cache c, int tokens, int tiles, const int32_t* __restrict__ i
     const int x = threadIdx.x + 256 * u, t = t0 + x / kChunks, ch = x % kChunks;
     to[u] = -1;
     if (t < count) {
-      kw[u] = *(const u32x4_t*)(k + from + (size_t)t * D + 8 * ch);
-      vw[u] = *(const u32x4_t*)(v + from + (size_t)t * D + 8 * ch);
+      kw[u] = __builtin_nontemporal_load((const u32x4_t*)(k + from + (size_t)t * D + 8 * ch));
+      vw[u] = __builtin_nontemporal_load((const u32x4_t*)(v + from + (size_t)t * D + 8 * ch));
       to[u] = slot_of(c, tables, s, first + t, h);
     }
   }
@@ -278,8 +281,8 @@ append_tile_kernel(Cache c, int tokens, int tiles, const int32_t* __restrict__ i
   for (int u = 0; u < kPer; ++u) {
     const int ch = (threadIdx.x + 256 * u) % kChunks;
     if (to[u] >= 0) {
-      *(u32x4_t*)(kp + to[u] + 8 * ch) = kw[u];
-      *(u32x4_t*)(vp + to[u] + 8 * ch) = vw[u];
+      __builtin_nontemporal_store(kw[u], (u32x4_t*)(kp + to[u] + 8 * ch));
+      __builtin_nontemporal_store(vw[u], (u32x4_t*)(vp + to[u] + 8 * ch));
     }
   }
 }
@@ -329,10 +332,10 @@ compact_move_kernel(Cache c, const int32_t* __restrict__ plan, const int32_t* __
     u32x4_t w[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (j0 + 256 * u < page) w[u] = from[j0 + 256 * u];
+      if (j0 + 256 * u < page) w[u] = __builtin_nontemporal_load(from + j0 + 256 * u);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (j0 + 256 * u < page) to[j0 + 256 * u] = w[u];
+      if (j0 + 256 * u < page) __builtin_nontemporal_store(w[u], to + j0 + 256 * u);
   }
 }
 
@@ -396,7 +399,7 @@ hipError_t launch_cache_reserve(const Cache& c, int n, const int32_t* ids, const
   reserve_plan_kernel<<<1, kPlan, 0, st>>>(c, n, ids, counts, tables, lens, refs, granted, w.src, w.copies);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(n, (unsigned)((c.planes * c.kv_heads + kCopyHeads - 1) / kCopyHeads));
+  const dim3 grid((unsigned)((c.planes * c.kv_heads + kCopyHeads - 1) / kCopyHeads), n);
   reserve_copy_kernel<<<grid, 256, 0, st>>>(c, w.copies, (uint16_t*)pool);
   return hipGetLastError();
 }
@@ -405,12 +408,12 @@ hipError_t launch_cache_append(const Cache& c, int n, int tokens, const int32_t*
                                const void* v, const int32_t* tables, const int32_t* lens, void* kp, void* vp, hipStream_t st) {
   const uint16_t *kk = (const uint16_t*)k, *vv = (const uint16_t*)v;
   uint16_t *ko = (uint16_t*)kp, *vo = (uint16_t*)vp;
-  if (tokens < kAppendTile) {
+  if (tokens < kManyTokens) {
     const int rows = n * c.kv_heads * tokens, per = 256 / (c.head_dim / 8);
     append_kernel<<<(unsigned)(((int64_t)rows + per - 1) / per), 256, 0, st>>>(c, rows, tokens, ids, counts, kk, vv, tables, lens, ko, vo);
     return hipGetLastError();
   }
-  const int tiles = (tokens + kAppendTile - 1) / kAppendTile;
+  const int tile = append_tile(c.head_dim), tiles = (tokens + tile - 1) / tile;
   const auto run = [&](auto kernel) {
     kernel<<<(unsigned)(n * c.kv_heads * tiles), 256, 0, st>>>(c, tokens, tiles, ids, counts, kk, vv, tables, lens, ko, vo);
     return hipGetLastError();

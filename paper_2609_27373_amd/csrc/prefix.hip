@@ -10,9 +10,12 @@
 // Results over disjoint ranges join as
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  O = sum O_i 2^(m_i - m),
 // so segments are cut along the keys into as many pieces as fill the chip:
-//   plan_kernel   finds the runs, cuts the segments, lists the pieces
-//   piece_kernel  one piece a work-group and key-value head: (m, l, O) in fp32
+//   piece_kernel  finds the runs, cuts the segments, and does a few pieces a
+//                 work-group: (m, l, O) in fp32
 //   join_kernel   joins the pieces of every row, divides by l
+//   plan_kernel   the runs and pieces of more than 256 sequences
+// Rounded to fewer bits than 32: the probabilities (bf16, where V is; at
+// most 1, the largest near it), and o.
 #include <algorithm>
 
 #include "plan.hpp"
@@ -41,41 +44,27 @@ struct Joint {
   int32_t own_slot, own_pieces, done, pad;   // done: a single piece wrote o
 };
 
-// Target numbers of work-groups, and the fewest keys of a piece.
-#ifndef GR
-#define GR 1024
-#endif
-#ifndef FK
-#define FK 128
-#endif
-#ifndef WG
-#define WG 256
-#endif
-#ifndef WK
-#define WK 768
-#endif
-constexpr int kGroups = GR, kFewKeys = FK;
-#ifndef HOLD
-#define HOLD (x.shared != nullptr ? 2 : D == 64 && NT == 1 ? 3 : 2)
-#endif
-#ifndef AHEAD
-#define AHEAD (D * NT <= 128)
-#endif
-#ifndef MK
-#define MK 512
-#endif
-#ifndef WR
-#define WR 64
-#endif
-constexpr int kWide = 128, kWideGroups = WG, kWideKeys = WK;   // the same for pieces of many rows
-constexpr int kPreTile = 32, kWideRows = WR;   // shared pages: rows of a piece of few rows, and of a segment up to which they are few
+// Sizes of the pieces.  Pieces of few rows: so many that there are kGroups / 2
+// (the work-groups that the chip holds at once), of at least kFewKeys keys; where
+// that makes them longer than kMidKeys, so many that there are kGroups.  us a call by the
+// number of pieces, 512 / 1024 / 2048: 8 samples of 4K, 55 heads of 96, 38 / 45 /
+// 54; 128 over a 32K prefix, 8 heads of 128, 279 / 265 / 263.
+constexpr int kGroups = 1024, kFewKeys = 128, kMidKeys = 512;
+// Pieces of up to 128 rows: kWideGroups, one a CU beside one of few rows, of at least
+// kWideKeys keys, since each leaves 128 rows of results to join.  64 / 128 / 256 / 512 of
+// them over the 32K prefix: 423 / 333 / 265 / 369 us; at least 256 / 512 / 768 / 1024
+// keys: 64.3 / 64.1 / 58.4 / 61.3 us at 64 over 8K, 33.4 / 31.8 / 32.7 / 36.6 at 16 x 5
+// drafts over 4K.
+constexpr int kWide = 128, kWideGroups = 256, kWideKeys = 768;
+// Shared pages: rows of a piece of few rows, and rows of a segment up to which it has few
+// (32 tasks' rows in pieces of 128: 28.7 us instead of 24.5).
+constexpr int kPreTile = 32, kWideRows = 64;
 
 // Who plans: nobody (every sequence is one piece), every work-group, a launch before.
 enum { kWhole, kOwnPlan, kPlanned };
-#ifndef WHOLE
-#define WHOLE 512
-#endif
-constexpr int kWholeKeys = WHOLE;      // most keys that are never cut
+// Most tokens of a table that are never cut, which saves the join: one sequence of 301
+// tokens, 8 heads of 64, 12 us instead of 19.
+constexpr int kWholeKeys = 512;
 
 struct Space {                         // the workspace
   int32_t* count;
@@ -147,8 +136,9 @@ struct Args {
 
 // ---------------------------------------------------------------------------
 // Plan: a thread a sequence.  Up to 256 sequences every work-group plans for
-// itself (its own piece is all it needs), which costs it less than a launch of
-// its own costs the call; more are planned by one group of 1024 threads.
+// itself, once for its few pieces (2 to 3 us, most of it the loads of ids and
+// lengths; a launch before it took 8 to 10), up to 64 in one wave without barriers;
+// more are planned by one group of 1024 threads.
 // ---------------------------------------------------------------------------
 template <int kN>
 struct Plan {                          // LDS
@@ -158,7 +148,6 @@ struct Plan {                          // LDS
   int32_t wave_sum[kN / 64][3], wave_start[kN / 64];
 };
 
-__device__ __forceinline__ int up_to(int64_t x, int y) { return (int)((x + y - 1) / y); }
 __device__ __forceinline__ int up_to(int x, int y) { return (int)(((uint32_t)x + y - 1) / (uint32_t)y); }
 
 // Pieces of `keys` keys when a piece should hold about `chunk`, and their even length.
@@ -174,8 +163,6 @@ __device__ __forceinline__ int known_len(const Args& x, int id) {
   return in_range(id, x.c.seqs) ? min(max(x.lens[id], 0), x.c.max_pages * x.c.page) : 0;
 }
 
-// Runs and pieces of all sequences: few and wides are the numbers of pieces of
-// either kind per key-value head.  Writes x.joint if `write`.
 // The planning threads are together: one wave needs no barrier for it.
 template <int kN>
 __device__ __forceinline__ void plan_sync() {
@@ -187,6 +174,8 @@ __device__ __forceinline__ void plan_sync() {
   }
 }
 
+// Runs and pieces of all sequences: few and wides are the numbers of pieces of
+// either kind per key-value head.  Writes x.joint if `write`.
 template <int kN>
 __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int& wides) {
   const int b = threadIdx.x, lane = b & 63, wave = kN > 64 ? b >> 6 : 0;
@@ -240,7 +229,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   auto even = [&](int64_t sum, int groups, int least) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
-  const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), MK));
+  const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), kMidKeys));
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
   cut_keys(leads ? pre : 0, wide ? even(k1, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
@@ -379,9 +368,11 @@ __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem)
 // a lane of one query, at keys 4 g .. 4 g + 3 of both 16-key halves (g = lane / 16).
 // The sum over keys in O^T = V^T P^T may run in any order, so these 8 are the
 // lane's slice of the B operand as they are, and its slice of V^T, the
-// same 8 keys at one dim, comes from loading D / 16 consecutive dims of each of the 8 keys
-// (a row of V per 16 lanes) and transposing within the lane: row m of the
-// t-th MFMA is dim (D / 16) m + t.  No LDS, no barrier until the four waves join.
+// same 8 keys at one dim, comes from loading D / 16 consecutive dims of each of the 8
+// keys (a row of V per 16 lanes, whole lines that are read once and need not stay in
+// the L2) and transposing within the lane: row m of the t-th MFMA is dim
+// (D / 16) m + t.  No LDS, no barrier until the four waves join.  Bound by
+// HBM: 32 sequences of up to 4K tokens, 8 heads of 128, 281 MB in 58 us (4.9 TB/s).
 // ---------------------------------------------------------------------------
 template <int D>
 struct VRow;
@@ -395,7 +386,7 @@ struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), alig
 template <int D, int NT>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int kh, float* lds) {
   constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT;
-  constexpr bool kAhead = AHEAD;
+  constexpr bool kAhead = D * NT <= 128;            // registers for a second V tile
   typedef typename VRow<D>::type VWords;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
@@ -454,7 +445,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
       bool ok;
       const uint16_t* base = x.vp + half_at(i, s, ok);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vr[4 * s + e] = *(const VWords*)(base + (4 * g + e) * D + kT * n);
+      for (int e = 0; e < 4; ++e) vr[4 * s + e] = __builtin_nontemporal_load((const VWords*)(base + (4 * g + e) * D + kT * n));
     }
   };
   if (tiles > 0) {
@@ -628,8 +619,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
 // A piece of up to 128 rows, all of which see all its keys (whole tiles of
 // 64): the software pipeline of the dense kernel (WaveRows::step), four waves
 // of 32 rows over rings of two K and two V tiles in LDS.  A wave copies 16
-// consecutive keys of a tile, which lie in one page.  False, with nothing
-// done, if some page id of the piece names no page.
+// consecutive keys of a tile, which lie in one page.  Bound by the matrix
+// cores and the exponentials, 1.3 us a tile of 64 keys of 128 beside a group of few
+// rows.  False, with nothing done, if some page id of the piece names no page.
 // ---------------------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh, char* smem) {
@@ -770,13 +762,16 @@ piece_kernel(Args x) {
     if (i > 0) __syncthreads();                     // the piece before has left the LDS
     if constexpr (kShared) {
       if (p.wide && tile_piece<D>(x, p, kh, smem)) continue;
+      if (p.see < 0x7fffffff - x.a.q_len) {
+        stream_piece<D, NT>(x, p, kh, (float*)smem);
+        continue;
+      }
       // A few rows, or, where a page is missing, many a few at a time.
       Piece s = p;
       for (int r = 0; r < p.rows; r += 32) {
         s.row0 = p.row0 + r;
         s.rows = min(32, p.rows - r);
-        if (NT == 2 || s.rows > 16) stream_piece<D, 2>(x, s, kh, (float*)smem);
-        else stream_piece<D, 1>(x, s, kh, (float*)smem);
+        stream_piece<D, 2>(x, s, kh, (float*)smem);
       }
     } else {
       stream_piece<D, NT>(x, p, kh, (float*)smem);
@@ -850,9 +845,10 @@ hipError_t launch(const Args& x, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  // As many groups as the chip holds at once (registers allow a CU so many),
-  // or as do all the pieces kTodo at a time.
-  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * HOLD;
+  // Two groups a CU (registers allow few kinds more, and three or four do worse where
+  // they do: 63 and 64 us instead of 58 at 32 sequences of up to 4K), or as many as do
+  // all the pieces kTodo at a time.
+  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * 2;
   const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
   if (x.shared != nullptr) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
   else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);

@@ -15,6 +15,7 @@
 namespace {
 
 constexpr int64_t kI32Max = 2147483647;
+constexpr int64_t kMaxTokens = 1 << 30;       // of a sequence in a paged cache
 constexpr int64_t kMaxPlaneHeads = 65535 * 16;   // a copy's grid has a row per 16 heads of all planes
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
@@ -62,8 +63,8 @@ wise_status check_cache(const wise_cache* c, wise::Cache* out) {
     return WISE_ERR_SHAPE;
   if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WISE_ERR_UNSUPPORTED;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return WISE_ERR_UNSUPPORTED;
-  // Token positions are int32; byte offsets into a pool are 64-bit.
-  if ((int64_t)c->max_pages * c->page > kI32Max || c->pages > wise::kMaxPages) return WISE_ERR_SHAPE;
+  // Token positions are int32, with room past the last one; byte offsets into a pool are 64-bit.
+  if ((int64_t)c->max_pages * c->page > kMaxTokens || c->pages > wise::kMaxPages) return WISE_ERR_SHAPE;
   if ((int64_t)c->kv_heads * c->page * c->head_dim > kI32Max || (int64_t)c->planes * c->kv_heads > kMaxPlaneHeads)
     return WISE_ERR_SHAPE;
   *out = wise::Cache{c->pages, c->page, c->kv_heads, c->head_dim, c->planes, c->seqs, c->max_pages};

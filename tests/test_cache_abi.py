@@ -58,7 +58,7 @@ CALLS = ("fork", "trim", "reserve", "append", "compact", "shared", "attn")
 @pytest.mark.parametrize("kw,status", [
     (dict(pages=0), SHAPE), (dict(page=-16), SHAPE), (dict(kv_heads=0), SHAPE), (dict(planes=0), SHAPE), (dict(seqs=-1), SHAPE),
     (dict(max_pages=0), SHAPE), (dict(page=8), UNSUPPORTED), (dict(page=48), UNSUPPORTED), (dict(page=256), UNSUPPORTED),
-    (dict(head_dim=80), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(max_pages=1 << 26), SHAPE), (dict(pages=(1 << 27) + 1), SHAPE),
+    (dict(head_dim=80), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(max_pages=1 << 26), SHAPE), (dict(max_pages=(1 << 25) + 1), SHAPE), (dict(planes=65536, kv_heads=17), SHAPE), (dict(pages=(1 << 27) + 1), SHAPE),
     (dict(kv_heads=1 << 20), SHAPE)])
 def test_geometry(fn, kw, status):
     assert call(fn, C(**kw)) == status
@@ -103,12 +103,20 @@ def test_sizes():
 @pytest.mark.parametrize("a,status", [
     (None, NULL), (wise.make_queries(0, 4), SHAPE), (wise.make_queries(2, 0), SHAPE), (wise.make_queries(2, 4, 0), SHAPE),
     (wise.make_queries(2, 3), SHAPE), (wise.make_queries(5, 4), SHAPE), (wise.make_queries(1025, 4), UNSUPPORTED),
-    (wise.make_queries(2, 4, 65), UNSUPPORTED), (wise.make_queries(2, 2 * 129), UNSUPPORTED), (wise.make_queries(2, 2, 1 << 30), UNSUPPORTED),
+    (wise.make_queries(2, 4, 65), UNSUPPORTED), (wise.make_queries(2, 2 * 129), UNSUPPORTED), (wise.make_queries(2, 2, 1 << 30), UNSUPPORTED), (wise.make_queries(1024, 1 << 16), UNSUPPORTED),
     (wise.make_queries(2, 4, 1, float("nan")), RANGE), (wise.make_queries(2, 4, 1, float("-inf")), RANGE)])
 def test_queries(a, status):
     assert call("attn", C(), a=a) == status
     if a is not None and a.batch != 5:
         assert wise.wise_prefix_workspace_bytes(C(), a) == 0
+
+
+def test_more_queries_than_indexes():
+    c = C(kv_heads=1 << 15, head_dim=64, page=16, seqs=1024)
+    assert call("attn", c, a=wise.make_queries(1024, 1 << 15)) == SHAPE          # 2^31 elements of q
+    assert wise.wise_prefix_workspace_bytes(c, wise.make_queries(1024, 1 << 15)) == 0
+    assert wise.wise_prefix_workspace_bytes(c, wise.make_queries(1023, 1 << 15)) > 0
+    assert wise.wise_cache_workspace_bytes(C(max_pages=1 << 25)) > 0
 
 
 def test_attention_workspace():

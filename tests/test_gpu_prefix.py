@@ -90,6 +90,29 @@ def test_lengths(gpu_lib, page, d, gq):
     b.check(*b.run(False))
 
 
+@pytest.mark.parametrize("page", [16, 64, 128])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("gq", [1, 4, 20])
+def test_lengths_beside_a_long_one(gpu_lib, page, d, gq):
+    """The same where sequences are cut and joined: a table of more than 512 tokens."""
+    tails = [None, 1, 16, 17, 63, 64, 65, 127, 128, 129, 256, 257, 1500, 33, None, 700]
+    b = Batch([(0, tails)], page, d, 2, gq, seed=page + d + gq)
+    b.check(*b.run(False))
+
+
+@pytest.mark.parametrize("batch", [63, 64, 65, 128, 200, 256, 257])
+def test_batch_sizes(gpu_lib, batch):
+    """Runs that cross the 64 sequences of a planning wave and the 256 of a work-group's own plan."""
+    rng = random.Random(batch)
+    groups, left = [], batch
+    while left:
+        n = min(left, rng.choice((1, 2, 30, 70)))
+        groups.append((rng.choice((4, 9, 44)) if n > 1 else 0, [rng.choice((None, 1, 20, 50)) if n < 30 else rng.randint(1, 50) for _ in range(n)]))
+        left -= n
+    b = Batch(groups, 16, 64, 2, 2, seed=batch, slots=True)
+    b.both()
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 @pytest.mark.parametrize("d", [64, 96, 128])
 @pytest.mark.parametrize("members", [2, 17, 40])
@@ -207,6 +230,74 @@ def test_bad_tables_and_lengths(gpu_lib):
     b.lens[full] = cols * 16 + 1000
     b.cache.lens.copy_(ints(b.lens.tolist()))
     b.both()
+
+
+def test_bad_page_shared_by_many(gpu_lib):
+    """A missing page under more rows than a piece of few has: those positions stay out for all of them."""
+    b = Batch([(40, [5, 9, 20] * 10)], 16, 64, 2, 4, seed=14)
+    for s in b.ids:
+        b.tables[s, 17] = -1
+        b.tables[s, 39] = b.pool.shape[1] + 5
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    b.both()
+
+
+@pytest.mark.parametrize("members", [3, 30])
+def test_infinite_shared_value(gpu_lib, members):
+    """An infinite value in a shared page reaches every row of its head, in its dim alone."""
+    b = Batch([(40, [5, 9, 20] * (members // 3))], 16, 96, 2, 4, seed=15)
+    ref, _ = b.run()
+    b.cache.pool[1, int(b.tables[b.ids[0], 12]), 1, 3, 50] = float("inf")
+    for shared in (True, False):
+        out, _ = b.run(shared)
+        assert not torch.isfinite(out[:, 4:, :, 50]).any()
+        keep = [i for i in range(96) if i != 50]
+        assert torch.isfinite(out[..., keep]).all() and torch.isfinite(out[:, :4]).all()
+        if shared:
+            assert torch.equal(out[..., keep], ref[..., keep]) and torch.equal(out[:, :4], ref[:, :4])
+
+
+def reference_on_gpu(q, k, v):
+    """(o, lse, bound, lse_bound) as cache_model.attend gives them, of rows q [rows][d] that see every key, by torch in fp64."""
+    d = q.shape[-1]
+    scale = float(np.float32(1 / np.sqrt(d)))
+    q, k, v = q.double(), k.double(), v.double()
+    x = (q @ k.t()) * scale
+    lse = torch.logsumexp(x, 1)
+    p = torch.exp(x - lse[:, None])
+    o = p @ v
+    e = scale * d * 2.0 ** -24 * (q.abs() @ k.abs().t()).amax(1, keepdim=True)
+    bound = 2.0 ** -8 * o.abs() + (1 + 2.0 ** -8) * (2.0 ** -8 + 2 * e + 2.0 ** -16) * (p @ v.abs())
+    return o, lse, bound, e[:, 0] + 2.0 ** -16 + 2.0 ** -22 * lse.abs()
+
+
+@pytest.mark.parametrize("batch,kv,gq,page,tokens", [(1, 16, 2, 128, 300001), (128, 8, 4, 64, 40000), (20, 8, 4, 16, 120000)])
+def test_pieces_of_more_than_4096_keys(gpu_lib, batch, kv, gq, page, tokens):
+    """So many keys that a piece is longer than the page ids that a wave holds at once, for one sequence and shared."""
+    d = 64
+    say(f"{batch} sequences over {tokens} tokens, {kv} heads")
+    g = torch.Generator(device="cuda").manual_seed(batch)
+    cols = up(tokens, page)
+    n = tokens // page * page                         # shared by all; each has up to a page of its own
+    pool = torch.randn((2, cols + batch, kv, page, d), generator=g, device="cuda").to(torch.bfloat16)
+    order = torch.randperm(cols + batch, generator=g, device="cuda").to(torch.int32)
+    tables = order[:cols][None].repeat(batch, 1)
+    tables[:, n // page:] = order[cols:cols + batch, None]
+    tables = tables[:, :up(tokens, page)].contiguous()
+    lens = torch.full((batch,), tokens, dtype=torch.int32, device="cuda")
+    c = PagedCache(1, cols + batch, page, kv, d, batch, tables.shape[1], pool=pool, tables=tables, lens=lens)
+    q = torch.randn((batch, kv * gq, 1, d), generator=g, device="cuda").to(torch.bfloat16)
+    shared = torch.full((batch,), n // page, dtype=torch.int32, device="cuda")
+    shared[0] = 0
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    c.attend(0, q, out, lse, shared=shared if batch > 1 else None)
+    for b in (0, batch - 1):
+        for h in (0, kv - 1):
+            k, v = (pool[x, tables[b].long(), h].reshape(-1, d)[:tokens] for x in (0, 1))
+            rows = slice(h * gq, (h + 1) * gq)
+            o, z, bound, zb = reference_on_gpu(q[b, rows, 0], k, v)
+            assert ((out[b, rows, 0].double() - o).abs() <= bound).all()
+            assert ((lse[b, rows, 0].double() - z).abs() <= zb).all()
 
 
 def test_repeated_and_foreign_ids(gpu_lib):
