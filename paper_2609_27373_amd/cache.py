@@ -30,6 +30,10 @@ from . import wise
 
 _I32, _BF16, _F32 = torch.int32, torch.bfloat16, torch.float32
 
+# The current stream's handle.  torch's public call builds a Stream object for it (1.2 us of the 7 of a call);
+# its own generated code asks for the handle alone.
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
 
 class PagedCache:
     def __init__(self, layers, pages, page, kv_heads, head_dim, seqs, max_pages, device="cuda", pool=None, tables=None,
@@ -84,15 +88,16 @@ class PagedCache:
         return t.data_ptr()
 
     def _call(self, fn, *args):
-        if self.device.type != "cuda":
-            raise ValueError("the cache is not on a GPU")
         index = self.device.index
+        if index is None:
+            raise ValueError("the cache is not on a GPU")
         entry = getattr(wise.load(), fn)
+        stream = _stream(index)
         if torch.cuda.current_device() == index:
-            status = entry(self._c, *args, torch.cuda.current_stream(index).cuda_stream)
+            status = entry(self._c, *args, stream)
         else:
             with torch.cuda.device(index):
-                status = entry(self._c, *args, torch.cuda.current_stream(index).cuda_stream)
+                status = entry(self._c, *args, stream)
         if status != 0:
             raise wise.WiseError(status, fn)
 

@@ -32,9 +32,12 @@ struct Piece {
   int32_t table;                       // table row with the segment's pages
   int32_t see;                         // positions that a sequence's first query sees
   int32_t slot;                        // row of the piece's results, key-value head 0, segment row 0; -1: the whole result, written to o
-  int32_t wide;                        // up to kWide rows, for tile_piece
-  int32_t pad[2];
+  int32_t kind, head;                  // head: key-value head, or group of four of them (kNarrow)
+  int32_t pad;
 };
+
+// Pieces of up to kWide rows; of few rows; of few rows and keys, a wave each.
+enum { kManyRows, kFewRows, kNarrow };
 
 // Where the pieces of a sequence's rows lie: results of row r over piece i of the
 // shared pages at pre_slot + (i * kv_heads + kh) * pre_rows + pre_row0 + r, over piece i of
@@ -59,6 +62,13 @@ constexpr int kWide = 128, kWideGroups = 256, kWideKeys = 768;
 // Shared pages: rows of a piece of few rows, and rows of a segment up to which it has few
 // (32 tasks' rows in pieces of 128: 28.7 us instead of 24.5).
 constexpr int kPreTile = 32, kWideRows = 64;
+// Where there are more (sequence, head)s than groups: keys of a sequence's own up to
+// which a wave takes them alone, four heads a group, since the latency of a piece is most of
+// its time (128 sequences of up to 64 tokens over a 16K prefix, 16 heads of 64: 40 us
+// instead of 49).
+constexpr int kNarrowKeys = 128, kHold = 512;
+
+constexpr int kSeeAll = 0x7fffffff - kMaxQueryRows;   // Piece::see of shared pages
 
 // Who plans: nobody (every sequence is one piece), every work-group, a launch before.
 enum { kWhole, kOwnPlan, kPlanned };
@@ -123,6 +133,7 @@ struct Args {
   int page_bits;
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
+  int narrow;                          // there may be pieces of a wave
   const uint16_t *q, *kp, *vp;
   const int32_t *tables, *lens, *ids, *shared;
   int32_t* count;
@@ -142,20 +153,25 @@ struct Args {
 // ---------------------------------------------------------------------------
 template <int kN>
 struct Plan {                          // LDS
-  int32_t members[kN], pre_keys[kN], see[kN], first[kN], wide_first[kN], id[kN], len[kN], own_len[kN], own_slot[kN], pre_slot[kN],
+  int32_t members[kN], pre_keys[kN], see[kN], first[3][kN], id[kN], len[kN], own_len[kN], own_slot[kN], pre_slot[kN],
       pre_pieces[kN], pre_len[kN];
   int64_t wave_keys[kN / 64][2];
-  int32_t wave_sum[kN / 64][3], wave_start[kN / 64];
+  int32_t wave_sum[kN / 64][4], wave_start[kN / 64];
+};
+
+struct Cuts {
+  int pieces[3];                       // of each kind, per key-value head (kNarrow: per four)
 };
 
 __device__ __forceinline__ int up_to(int x, int y) { return (int)(((uint32_t)x + y - 1) / (uint32_t)y); }
 
-// Pieces of `keys` keys when a piece should hold about `chunk`, and their even length.
+// Pieces of `keys` keys when a piece should hold about `chunk`, and their even length
+// (pieces of `chunk` and a rest: 265 us instead of 254 at 128 sequences over 32K).
 __device__ __forceinline__ void cut_keys(int keys, int chunk, int unit, int& pieces, int& len) {
   pieces = 0;
   len = unit;
   if (keys <= 0) return;
-  len = up_to(up_to(keys, up_to(keys, chunk)), unit) * unit;
+  len = (up_to(keys, up_to(keys, chunk)) + unit - 1) & -unit;
   pieces = up_to(keys, len);
 }
 
@@ -174,10 +190,9 @@ __device__ __forceinline__ void plan_sync() {
   }
 }
 
-// Runs and pieces of all sequences: few and wides are the numbers of pieces of
-// either kind per key-value head.  Writes x.joint if `write`.
+// Runs and pieces of all sequences.  Writes x.joint if `write`.
 template <int kN>
-__device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int& wides) {
+__device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
   const int b = threadIdx.x, lane = b & 63, wave = kN > 64 ? b >> 6 : 0;
   const Cache& c = x.c;
   const Queries& a = x.a;
@@ -210,7 +225,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
   const bool leads = live && b == start && pre > 0;
   const int pre_rows = leads ? n * rows : 0;
   const bool wide = pre_rows > kWideRows;
-  const int pre_tiles = up_to(pre_rows, wide ? kWide : kPreTile);
+  const int pre_tiles = wide ? (pre_rows + kWide - 1) / kWide : (pre_rows + kPreTile - 1) / kPreTile;
   int64_t k0 = (int64_t)own_tiles * own + (wide ? 0 : (int64_t)pre_tiles * pre), k1 = wide ? (int64_t)pre_tiles * pre : 0;
   k0 = wave_total(k0);
   k1 = x.shared != nullptr ? wave_total(k1) : 0;
@@ -227,40 +242,48 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
     }
   }
   auto even = [&](int64_t sum, int groups, int least) {
-    return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
+    return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 29);
   };
   const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), kMidKeys));
+  const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
   cut_keys(leads ? pre : 0, wide ? even(k1, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
-  // Prefix sums: pieces of few rows, of many, rows of results.
-  const int mine[3] = {own_n * own_tiles + (wide ? 0 : pre_n * pre_tiles), wide ? pre_n * pre_tiles : 0,
+  // Prefix sums: pieces of each kind, rows of results.
+  const int own_all = own_n * own_tiles, pre_all = pre_n * pre_tiles;
+  const int mine[4] = {wide ? pre_all : 0, (narrow ? 0 : own_all) + (wide ? 0 : pre_all), narrow ? own_all : 0,
                        (done ? 0 : own_n * c.kv_heads * rows) + pre_n * c.kv_heads * pre_rows};
-  int sum[3] = {wave_scan_add(mine[0]), x.shared != nullptr ? wave_scan_add(mine[1]) : 0, wave_scan_add(mine[2])};
+  int sum[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = wave_scan_add(mine[i]);
   if constexpr (kN > 64) {
     if (lane == 63)
 #pragma unroll
-      for (int i = 0; i < 3; ++i) s.wave_sum[wave][i] = sum[i];
+      for (int i = 0; i < 4; ++i) s.wave_sum[wave][i] = sum[i];
     __syncthreads();
-    few = wides = 0;
+    int all[4] = {0, 0, 0, 0};
     for (int w = 0; w < kN / 64; ++w) {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) sum[i] += w < wave ? s.wave_sum[w][i] : 0;
-      few += s.wave_sum[w][0];
-      wides += s.wave_sum[w][1];
+      for (int i = 0; i < 4; ++i) {
+        const int y = s.wave_sum[w][i];
+        sum[i] += w < wave ? y : 0;
+        all[i] += y;
+      }
     }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) cut.pieces[i] = all[i];
   } else {
-    few = __builtin_amdgcn_readlane(sum[0], 63);
-    wides = __builtin_amdgcn_readlane(sum[1], 63);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) cut.pieces[i] = __builtin_amdgcn_readlane(sum[i], 63);
   }
-  s.first[b] = sum[0] - mine[0];
-  s.wide_first[b] = sum[1] - mine[1];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) s.first[i][b] = sum[i] - mine[i];
+  s.pre_slot[b] = sum[3] - mine[3];
+  s.own_slot[b] = done ? -1 : sum[3] - mine[3] + pre_n * c.kv_heads * pre_rows;
   s.id[b] = id;
   s.len[b] = len;
   s.own_len[b] = own_l;
-  s.pre_slot[b] = sum[2] - mine[2];
-  s.own_slot[b] = done ? -1 : sum[2] - mine[2] + pre_n * c.kv_heads * pre_rows;
   s.pre_pieces[b] = pre_n;
   s.pre_len[b] = pre_l;
   if (x.shared == nullptr) s.members[b] = 1;
@@ -270,28 +293,29 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, int& few, int&
     x.joint[b] = Joint{s.pre_slot[start], pre > 0 ? s.pre_pieces[start] : 0, n * rows, (b - start) * rows, s.own_slot[b], own_n, done, 0};
 }
 
-// Piece k of a plan: those of many rows first.
+// Piece j of a kind.
 template <int kN>
-__device__ Piece piece_at(const Args& x, const Plan<kN>& s, int wides, int k) {
+__device__ Piece piece_at(const Args& x, const Plan<kN>& s, int kind, int j) {
   const int rows = x.rows, kv = x.c.kv_heads;
+  const int e = plan_entry<kN>(s.first[kind], j);
+  j -= s.first[kind][e];
   Piece p;
-  p.wide = k < wides;
-  const int32_t* first = p.wide ? s.wide_first : s.first;
-  int j = p.wide ? k : k - wides;
-  const int e = plan_entry<kN>(first, j);
-  j -= first[e];
-  const int pre_rows = s.pre_pieces[e] > 0 ? s.members[e] * rows : 0;
-  int tile = p.wide ? kWide : kPreTile;
-  const int pre_tiles = up_to(pre_rows, tile), pre_all = p.wide || pre_rows <= kWideRows ? s.pre_pieces[e] * pre_tiles : 0;
+  p.kind = kind;
   p.first = e;
   p.table = s.id[e];
+  const int pre_rows = s.pre_pieces[e] > 0 ? s.members[e] * rows : 0;
+  const bool pre_wide = pre_rows > kWideRows;
+  const int pre_tiles = pre_wide ? (pre_rows + kWide - 1) / kWide : (pre_rows + kPreTile - 1) / kPreTile;
+  const int pre_all = kind == kManyRows || (kind == kFewRows && !pre_wide) ? s.pre_pieces[e] * pre_tiles : 0;
+  int tile;
   if (j < pre_all) {
-    const int i = (uint32_t)j / (uint32_t)pre_tiles;
+    const int i = (uint32_t)j / (uint32_t)pre_tiles, len = s.pre_len[e];
+    tile = pre_wide ? kWide : kPreTile;
     p.seg_rows = pre_rows;
     p.row0 = (j - i * pre_tiles) * tile;
-    p.k0 = i * s.pre_len[e];
-    p.k1 = min(p.k0 + s.pre_len[e], s.pre_keys[e]);
-    p.see = 0x7fffffff - x.a.q_len;
+    p.k0 = i * len;
+    p.k1 = min(p.k0 + len, s.pre_keys[e]);
+    p.see = kSeeAll;
     p.slot = s.pre_slot[e] + i * kv * pre_rows;
   } else {
     j -= pre_all;
@@ -305,57 +329,86 @@ __device__ Piece piece_at(const Args& x, const Plan<kN>& s, int wides, int k) {
     p.slot = s.own_slot[e] < 0 ? -1 : s.own_slot[e] + i * kv * rows;
   }
   p.rows = min(tile, p.seg_rows - p.row0);
-  p.pad[0] = p.pad[1] = 0;
+  p.pad = 0;
   return p;
+}
+
+// Kind of piece k of all, in the order of the kinds; k becomes its number in the kind.
+__device__ __forceinline__ int kind_of(const Cuts& cut, int& k) {
+  int kind = kManyRows;
+  if (k >= cut.pieces[kManyRows]) {
+    k -= cut.pieces[kManyRows];
+    kind = kFewRows;
+    if (k >= cut.pieces[kFewRows]) {
+      k -= cut.pieces[kFewRows];
+      kind = kNarrow;
+    }
+  }
+  return kind;
 }
 
 __global__ void __launch_bounds__(kPlan)
 plan_kernel(Args x) {
   __shared__ Plan<kPlan> s;
-  int few, wides;
-  make_plan<kPlan>(x, s, true, few, wides);
-  const int all = min(few + wides, x.most);
-  if (threadIdx.x == 0) *x.count = all;
-  for (int k = threadIdx.x; k < all; k += kPlan) x.piece[k] = piece_at<kPlan>(x, s, wides, k);
+  Cuts cut;
+  make_plan<kPlan>(x, s, true, cut);
+  const int all = min(cut.pieces[0] + cut.pieces[1] + cut.pieces[2], x.most);
+  if (threadIdx.x < 3) x.count[threadIdx.x] = cut.pieces[threadIdx.x];
+  for (int k = threadIdx.x; k < all; k += kPlan) {
+    int j = k;
+    const int kind = kind_of(cut, j);
+    x.piece[k] = piece_at<kPlan>(x, s, kind, j);
+  }
 }
 
-// The pieces that this work-group is to do, in todo[0 .. count - 1], the key-value head
-// of each in pad[0]; returns the count.  The (piece, head)s are dealt to the groups in turn,
-// there and back, so that a group plans once and does a few, and the last ones
-// go to the groups that began with the lightest.
+// The pieces that this work-group is to do, in todo[0 .. count - 1]; returns the
+// count.  The (piece, head)s are dealt to the groups in turn, there and back, those of
+// many rows first: a group plans once and does a few, and the last ones go to the
+// groups that began with the lightest.
 constexpr int kTodo = 8;
 
 __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem) {
-  const uint32_t kv = x.c.kv_heads;
-  int few = 0, wides = 0;
+  const int kv = x.c.kv_heads, fours = (kv + 3) / 4;
+  Cuts cut{};
   const bool one_wave = x.a.batch <= 64;
   if (x.mode == kOwnPlan) {
-    if (!one_wave) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, few, wides);
-    else if (threadIdx.x < 64) make_plan<64>(x, *(Plan<64>*)smem, blockIdx.x == 0, few, wides);
+    if (!one_wave) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, cut);
+    else if (threadIdx.x < 64) make_plan<64>(x, *(Plan<64>*)smem, blockIdx.x == 0, cut);
+  } else if (x.mode == kPlanned) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) cut.pieces[i] = x.count[i];
+  } else {
+    cut.pieces[x.narrow ? kNarrow : kFewRows] = x.most;
   }
-  const int64_t all = (int64_t)(x.mode == kOwnPlan ? min(few + wides, x.most) : x.mode == kPlanned ? *x.count : x.most) * kv;
+  const int64_t whole = (int64_t)(cut.pieces[kManyRows] + cut.pieces[kFewRows]) * kv, all = whole + (int64_t)cut.pieces[kNarrow] * fours;
   const int64_t f = (int64_t)threadIdx.x * gridDim.x + (threadIdx.x % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
   if (threadIdx.x < kTodo && f < all) {
-    const int k = (int)((uint32_t)f / kv);
+    const uint32_t at = (uint32_t)(f < whole ? f : f - whole), heads = f < whole ? kv : fours;
+    int k = (int)(at / heads);
+    const int head = (int)(at - k * heads);
+    if (f >= whole) k += cut.pieces[kManyRows] + cut.pieces[kFewRows];
     Piece p;
-    if (x.mode == kOwnPlan) {
-      p = one_wave ? piece_at<64>(x, *(Plan<64>*)smem, wides, k) : piece_at<256>(x, *(Plan<256>*)smem, wides, k);
-    } else if (x.mode == kPlanned) {
+    if (x.mode == kPlanned) {
       p = x.piece[k];
-    } else {                                        // kWhole: a sequence's rows against all its keys
-      p.first = x.tiles == 1 ? k : (int)((uint32_t)k / (uint32_t)x.tiles);
-      p.seg_rows = x.rows;
-      p.row0 = (k - p.first * x.tiles) * x.tile;
-      p.rows = min(x.tile, x.rows - p.row0);
-      const int id = x.ids ? x.ids[p.first] : p.first;
-      p.k0 = 0;
-      p.k1 = known_len(x, id);
-      p.table = in_range(id, x.c.seqs) ? id : 0;
-      p.see = p.k1 - x.a.q_len + 1;
-      p.slot = -1;
-      p.wide = 0;
+    } else {
+      const int kind = kind_of(cut, k);
+      if (x.mode == kOwnPlan) {
+        p = one_wave ? piece_at<64>(x, *(Plan<64>*)smem, kind, k) : piece_at<256>(x, *(Plan<256>*)smem, kind, k);
+      } else {                                      // kWhole: a sequence's rows against all its keys
+        p.first = x.tiles == 1 ? k : (int)((uint32_t)k / (uint32_t)x.tiles);
+        p.seg_rows = x.rows;
+        p.row0 = (k - p.first * x.tiles) * x.tile;
+        p.rows = min(x.tile, x.rows - p.row0);
+        const int id = x.ids ? x.ids[p.first] : p.first;
+        p.k0 = 0;
+        p.k1 = known_len(x, id);
+        p.table = in_range(id, x.c.seqs) ? id : 0;
+        p.see = p.k1 - x.a.q_len + 1;
+        p.slot = -1;
+        p.kind = kind;
+      }
     }
-    p.pad[0] = (int)((uint32_t)f - (uint32_t)k * kv);
+    p.head = head;
     todo[threadIdx.x] = p;
   }
   return __syncthreads_count(threadIdx.x < kTodo && f < all);
@@ -383,14 +436,27 @@ struct VRow<96> { typedef uint32_t type __attribute__((ext_vector_type(3), align
 template <>
 struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(16))); };
 
-template <int D, int NT>
-__device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int kh, float* lds) {
+// threadIdx.x, unknown to the compiler: what a piece computes from it would else be
+// kept in registers over the loop over pieces, for every kind of piece at once (56
+// registers spilled at D = 128, 66 us instead of 54 at 64 sequences over 8K).
+__device__ __forceinline__ int fresh_tid() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
+template <int D, int NT, bool kAlone>
+__device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, float* lds) {
   constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT;
   constexpr bool kAhead = D * NT <= 128;            // registers for a second V tile
   typedef typename VRow<D>::type VWords;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int rows = x.rows, page = x.c.page;
+  // The four waves share the piece, or (kAlone) each has its own, of the next head.
+  constexpr int stride = kAlone ? 32 : 128;
+  const int begin = p.k0 + (kAlone ? 0 : 32 * wave);
+  const int my_head = kAlone ? 4 * p.head + wave : p.head, kh = min(my_head, x.c.kv_heads - 1);
   const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
   u32x4_t qf[NT][kC];
   int see[NT];
@@ -414,10 +480,10 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
     for (int t = 0; t < kT; ++t) o[u][t] = f32x4_t{};
   }
   // Page ids of this wave's tiles: lane 2 i + s has the one of half s of tile i (mod 32), -1 for none.
-  const int tiles = (p.k1 - p.k0 - 32 * wave + 127) / 128;
+  const int tiles = my_head < x.c.kv_heads ? (p.k1 - begin + stride - 1) / stride : 0;
   int ids = -1;
   auto load_ids = [&](int i0) {
-    const int key = p.k0 + 32 * wave + 128 * (i0 + (lane >> 1)) + 16 * (lane & 1);
+    const int key = begin + stride * (i0 + (lane >> 1)) + 16 * (lane & 1);
     ids = key < p.k1 ? table[key >> x.page_bits] : -1;
     if (!in_range(ids, x.c.pages)) ids = -1;
   };
@@ -426,7 +492,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   uint32_t poison = 0;                              // infinite or NaN values set aside
   auto half_at = [&](int i, int s, bool& ok) {      // element offset of half s of tile i
     const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + s);
-    const int key = p.k0 + 32 * wave + 128 * i + 16 * s;
+    const int key = begin + stride * i + 16 * s;
     ok = id >= 0;
     return (((size_t)(ok ? id : 0) * x.c.kv_heads + kh) * page + (key & (page - 1))) * D;
   };
@@ -455,7 +521,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
   }
   // Tile i, its V in vr; the next tile's K and V (into vn) are loaded meanwhile.
   auto tile = [&](int i, VWords (&vr)[8], VWords (&vn)[8]) {
-    const int key0 = p.k0 + 32 * wave + 128 * i;
+    const int key0 = begin + stride * i;
     bool ok0, ok1;
     half_at(i, 0, ok0);
     half_at(i, 1, ok1);
@@ -578,15 +644,20 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
       for (int t = 0; t < kT; t += 2) *(f32x2_t*)(lds + r * kStride + kT * (4 * g + i) + t) = f32x2_t{o[u][t][i], o[u][t + 1][i]};
   }
   __syncthreads();
-  for (int j = tid; j < p.rows * (D / 4); j += 256) {
+  if (my_head >= x.c.kv_heads) return;
+  for (int j = kAlone ? lane : tid; j < p.rows * (D / 4); j += kAlone ? 64 : 256) {
     const int r = j / (D / 4), d = j % (D / 4) * 4;
     float mw[4], mx = -INFINITY, lt = 0.f;
     f32x4_t sum{};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, mw[w] = mls[2 * (w * kRows + r)]);
+    for (int w = 0; w < 4; ++w) {
+      mw[w] = kAlone && w != wave ? -INFINITY : mls[2 * (w * kRows + r)];
+      mx = fmaxf(mx, mw[w]);
+    }
     const float mb = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
+      if (kAlone && w != wave) continue;
       const float f = fast_exp2(mw[w] - mb);
       lt += f * mls[2 * (w * kRows + r) + 1];
       sum += f * *(const f32x4_t*)(lds + (w * kRows + r) * kStride + d);
@@ -624,11 +695,11 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, int 
 // rows.  False, with nothing done, if some page id of the piece names no page.
 // ---------------------------------------------------------------------------
 template <int D>
-__device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh, char* smem) {
+__device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* smem) {
   using G = Geo<D>;
   constexpr int kT = Swizzle<D>::kTile, kC = TileCopy<D, 4>::kPer;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = x.rows, page = x.c.page;
+  const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = x.rows, page = x.c.page, kh = p.head;
   const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
   const int tiles = (p.k1 - p.k0) / kKeyTile;
   // Page ids of this wave's keys: lane i has the one of tile 64 u + i, of stretch u and the next one.
@@ -637,6 +708,9 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh
     return key < p.k1 ? table[key >> x.page_bits] : 0;
   };
   int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
+  bool bad = false;
+  for (int j = (p.k0 >> x.page_bits) + tid; j <= (p.k1 - 1) >> x.page_bits; j += 256) bad |= !in_range(table[j], x.c.pages);
+  if (__syncthreads_or(bad)) return false;
   WaveRows<D> w;
   w.reset();
   {
@@ -646,9 +720,6 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, int kh
 #pragma unroll
     for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
   }
-  bool bad = false;
-  for (int j = (p.k0 >> x.page_bits) + tid; j <= (p.k1 - 1) >> x.page_bits; j += 256) bad |= !in_range(table[j], x.c.pages);
-  if (__syncthreads_or(bad)) return false;
   TileCopy<D, 4> cp;
   ReadAddr<D> ra;
   cp.init(wave, lane);
@@ -758,12 +829,12 @@ piece_kernel(Args x) {
     int32_t* w = (int32_t*)&p;                     // the same in every lane
 #pragma unroll
     for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
-    const int kh = p.pad[0];
     if (i > 0) __syncthreads();                     // the piece before has left the LDS
     if constexpr (kShared) {
-      if (p.wide && tile_piece<D>(x, p, kh, smem)) continue;
-      if (p.see < 0x7fffffff - x.a.q_len) {
-        stream_piece<D, NT>(x, p, kh, (float*)smem);
+      if (p.kind == kManyRows && tile_piece<D>(x, p, smem)) continue;
+      if (p.see != kSeeAll) {
+        if (p.kind == kNarrow) stream_piece<D, NT, true>(x, p, (float*)smem);
+        else stream_piece<D, NT, false>(x, p, (float*)smem);
         continue;
       }
       // A few rows, or, where a page is missing, many a few at a time.
@@ -771,10 +842,11 @@ piece_kernel(Args x) {
       for (int r = 0; r < p.rows; r += 32) {
         s.row0 = p.row0 + r;
         s.rows = min(32, p.rows - r);
-        stream_piece<D, 2>(x, s, kh, (float*)smem);
+        stream_piece<D, 2, false>(x, s, (float*)smem);
       }
     } else {
-      stream_piece<D, NT>(x, p, kh, (float*)smem);
+      if (p.kind == kNarrow) stream_piece<D, NT, true>(x, p, (float*)smem);
+      else stream_piece<D, NT, false>(x, p, (float*)smem);
     }
   }
 }
@@ -848,7 +920,7 @@ hipError_t launch(const Args& x, hipStream_t st) {
   // Two groups a CU (registers allow few kinds more, and three or four do worse where
   // they do: 63 and 64 us instead of 58 at 32 sequences of up to 4K), or as many as do
   // all the pieces kTodo at a time.
-  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = 256 * 2;
+  const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = kHold;
   const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
   if (x.shared != nullptr) piece_kernel<D, NT, true><<<grid, 256, 0, st>>>(x);
   else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
@@ -876,6 +948,7 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
   x.rows = a.heads / c.kv_heads * a.q_len;
   x.tiles = (x.rows + x.tile - 1) / x.tile;
   x.page_bits = __builtin_ctz(c.page);
+  x.narrow = (int64_t)a.batch * c.kv_heads > kHold;
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;
   x.q = (const uint16_t*)q, x.kp = (const uint16_t*)kp, x.vp = (const uint16_t*)vp;
   x.tables = tables, x.lens = lens, x.ids = ids, x.shared = shared;

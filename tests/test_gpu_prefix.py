@@ -113,6 +113,18 @@ def test_batch_sizes(gpu_lib, batch):
     b.both()
 
 
+@pytest.mark.parametrize("d,kv,gq,q_len", [(64, 5, 1, 1), (96, 3, 4, 3), (128, 8, 5, 4), (64, 6, 20, 2)])
+@pytest.mark.parametrize("longest", [100, 400, 2000])
+def test_more_heads_than_groups(gpu_lib, d, kv, gq, q_len, longest):
+    """So many sequences and heads that short tails are a wave's each, four heads a group; heads that 4 does not
+    divide, tails on both sides of what a wave takes, whole tables that are never cut."""
+    rng = random.Random(d + kv)
+    tails = [rng.choice((None, 1, 2, q_len, 31, 32, 33, 64, 100, 127, 128, 129, 160)) for _ in range(600 // kv)]
+    tails = [x if x is None else min(x, longest) for x in tails] + [longest]
+    b = Batch([(0, tails[:40]), (3, tails[40:60]), (0, tails[60:])], 32, d, kv, gq, q_len, seed=longest)
+    b.both()
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 @pytest.mark.parametrize("d", [64, 96, 128])
 @pytest.mark.parametrize("members", [2, 17, 40])
