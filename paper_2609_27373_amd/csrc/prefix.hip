@@ -242,7 +242,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
     }
   }
   auto even = [&](int64_t sum, int groups, int least) {
-    return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 29);
+    return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
   const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), kMidKeys));
   const bool narrow = x.narrow && own <= kNarrowKeys;

@@ -222,6 +222,20 @@ def test_infinite_keys_and_values(gpu_lib):
         assert torch.equal(out[rest], ref[rest]), bad
 
 
+@pytest.mark.parametrize("members", [4, 40])
+def test_nan_query(gpu_lib, members):
+    """A NaN in one query makes that row NaN and changes no bit of the others."""
+    b = Batch([(30, [5, 70, 200, 33] * (members // 4))], 16, 128, 2, 4, seed=16)
+    refs = [b.run(shared)[0] for shared in (True, False)]
+    b.q[1, 5, 0, 100] = float("nan")
+    for shared, ref in zip((True, False), refs):
+        out, lse = b.run(shared)
+        rest = torch.ones(out.shape[:3], dtype=torch.bool, device="cuda")
+        rest[1, 5, 0] = False
+        assert torch.isnan(out[1, 5, 0]).all() and torch.isnan(lse[1, 5, 0])
+        assert torch.equal(out[rest], ref[rest])
+
+
 def test_bad_tables_and_lengths(gpu_lib):
     """Page ids outside the pool are not read, their positions not attended; lengths past the table and below 0 are cut."""
     b = Batch([(4, [30, 70, 20, 40]), (0, [100])], 16, 64, 1, 4, seed=4)
