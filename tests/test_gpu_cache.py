@@ -286,3 +286,75 @@ def test_a_step_in_a_graph(gpu_lib):
         if rep % 2:
             grow(c, m, [0], [1], seed=rep)            # eager work between replays
             same(c, m)
+
+
+def test_binding_functions(gpu_lib):
+    """The binding's functions, one per C entry point, on the caller's own buffers and on a stream that is passed in."""
+    w = gpu_lib
+    c = w.make_cache(30, 16, 2, 64, 2, 6, 8)
+    m = Model(2, 30, 16, 2, 64, 6, 8, np.zeros((2, 30, 2, 16, 64), np.int16))
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        pool = torch.zeros((2, 30, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
+        tables, lens, refs = torch.full((6, 8), -1, dtype=torch.int32, device="cuda"), ints([0] * 6), ints([0] * 30)
+        ws = torch.empty(w.wise_cache_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+        a = w.make_queries(2, 4)
+        aws = torch.empty(w.wise_prefix_workspace_bytes(c, a), dtype=torch.uint8, device="cuda")
+        granted, done, shared, live = ints([0] * 2), ints([0] * 2), ints([0] * 2), ints([0])
+        k, v = (torch.randint(-2 ** 14, 2 ** 14, (2, 2, 40, 64), dtype=torch.int16, generator=torch.Generator().manual_seed(i)) for i in (1, 2))
+        kd, vd, q = k.cuda().view(torch.bfloat16), v.cuda().view(torch.bfloat16), torch.randn(2, 4, 1, 64, device="cuda").to(torch.bfloat16)
+        out, lse = torch.empty_like(q), torch.empty((2, 4, 1), device="cuda")
+    w.wise_cache_reserve(c, ints([1, 4]), ints([40, 21]), tables, lens, refs, granted, pool, ws, stream=st)
+    w.wise_cache_append(c, 40, ints([1, 4]), granted, kd, vd, tables, lens, pool[0], pool[1], stream=st)
+    w.wise_cache_fork(c, ints([1, 4]), ints([0, 5]), tables, lens, refs, done, stream=st)
+    w.wise_cache_trim(c, ints([4, 1]), ints([0, 17]), tables, lens, refs, stream=st)
+    w.wise_cache_compact(c, tables, refs, pool, live, ws, stream=st)
+    w.wise_cache_shared(c, 2, 1, ints([0, 1]), tables, lens, shared, stream=st)
+    w.wise_prefix_attn(c, a, q, pool[0], pool[1], tables, lens, ints([0, 1]), shared, out, lse, aws, stream=st)
+    want = m.reserve([1, 4], [40, 21])
+    m.append(0, k.numpy(), v.numpy(), [1, 4], want)
+    assert m.fork([1, 4], [0, 5]) == [1, 1]
+    m.trim([4, 1], [0, 17])
+    pages = m.compact()
+    st.synchronize()
+    assert granted.cpu().tolist() == want and done.cpu().tolist() == [1, 1] and live.cpu().tolist() == [pages]
+    assert tables.cpu().tolist() == m.tables and lens.cpu().tolist() == m.lens and refs.cpu().tolist() == m.refs
+    assert np.array_equal(bits(pool), m.pool) and shared.cpu().tolist() == m.shared([0, 1]) == [0, 1]
+    again = PagedCache(1, 30, 16, 2, 64, 6, 8, pool=pool, tables=tables, lens=lens, refs=refs)
+    out2 = again.attend(0, q, torch.empty_like(q), seq_ids=ints([0, 1]), shared=shared)
+    # the keys are any bits, NaN among them: the same bits, from the same kernels
+    assert np.array_equal(bits(out), bits(out2))
+    with pytest.raises(w.WiseError):
+        w.wise_prefix_attn(c, a, q, pool[0], pool[1], tables, lens, None, None, out, lse, aws[:256])
+    with pytest.raises(w.WiseError):
+        w.wise_prefix_attn(c, a, q, pool[0], pool[1], tables, lens, None, None, out, lse, None)
+    for bad in (dict(q=q.float()), dict(q=q[:1]), dict(seq_ids=ints([0])), dict(seq_ids=torch.zeros(2, dtype=torch.int64, device="cuda"))):
+        args = dict(dict(q=q, seq_ids=ints([0, 1])), **bad)
+        with pytest.raises(ValueError):
+            w.wise_prefix_attn(c, a, args["q"], pool[0], pool[1], tables, lens, args["seq_ids"], None, out, lse, aws)
+
+
+def test_paged_cache_arguments(gpu_lib):
+    """What PagedCache refuses before any launch: types, sizes, strides, devices, layers."""
+    c, m = pair()
+    grow(c, m, [0], [20])
+    q = torch.zeros((1, 4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    good = dict(q=q, out=torch.empty_like(q))
+    c.attend(0, **good)
+    c.attend(0, q.view(1, 1, 4, 64).transpose(1, 2), good["out"])     # strides of dims of one do not matter
+    for bad in (dict(q=q.half()), dict(out=torch.empty_like(q).float()), dict(seq_ids=torch.tensor([0], device="cuda")),
+                dict(seq_ids=torch.tensor([0], dtype=torch.int32)), dict(shared=ints([])), dict(lse=torch.empty(4, device="cuda", dtype=torch.float64)),
+                dict(lse=torch.empty(3, device="cuda")), dict(q=torch.zeros((1, 4, 1, 128), dtype=torch.bfloat16, device="cuda")[..., ::2])):
+        with pytest.raises(ValueError):
+            c.attend(0, **dict(good, **bad))
+    with pytest.raises(ValueError):
+        c.attend(1, **good)
+    for call in (lambda: c.fork(ints([0]), ints([])), lambda: c.trim(torch.tensor([0], device="cuda")), lambda: c.reserve(ints([0, 1]), ints([1])),
+                 lambda: c.shared(out=ints([0])), lambda: c.append(0, *kv_rows(c, 1, 1, 0), ints([0]), ints([1]))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(gpu_lib.WiseError):
+        c.attend(0, torch.zeros((1, 3, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((1, 3, 1, 64), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(gpu_lib.WiseError):
+        c.trim(torch.zeros(1025, dtype=torch.int32, device="cuda"))
+    same(c, m)
