@@ -53,12 +53,13 @@ struct Joint {
 // number of pieces, 512 / 1024 / 2048: 8 samples of 4K, 55 heads of 96, 38 / 45 /
 // 54; 128 over a 32K prefix, 8 heads of 128, 279 / 265 / 263.
 constexpr int kGroups = 1024, kFewKeys = 128, kMidKeys = 512;
-// Pieces of up to 128 rows: kWideGroups, one a CU beside one of few rows, of at least
-// kWideKeys keys, since each leaves 128 rows of results to join.  64 / 128 / 256 / 512 of
-// them over the 32K prefix: 423 / 333 / 265 / 369 us; at least 256 / 512 / 768 / 1024
-// keys: 64.3 / 64.1 / 58.4 / 61.3 us at 64 over 8K, 33.4 / 31.8 / 32.7 / 36.6 at 16 x 5
-// drafts over 4K.
-constexpr int kWide = 128, kWideGroups = 256, kWideKeys = 768;
+// Pieces of up to 128 rows: at most kWideGroups, one a CU beside one of few rows, and of at
+// most kWideKeys keys where that leaves kWideFill, since each leaves 128 rows of results to
+// join; of at least kWideLeast keys.  64 / 128 / 256 / 512 of them over the 32K prefix: 423 / 333
+// / 265 / 369 us; at least 256 / 512 / 768 / 1024 keys: 64.3 / 64.1 / 58.4 / 61.3 us at 64
+// sequences over 8K; filled up to 192 of them, not left at 768 keys each: 24.0 instead of 28.8 us
+// at 40 over 2K, 19.0 instead of 21.8 at 16 over 4K, 31.5 instead of 32.8 at 16 x 5 drafts over 4K.
+constexpr int kWide = 128, kWideGroups = 256, kWideFill = 192, kWideKeys = 768, kWideLeast = 256;
 // Shared pages: rows of a piece of few rows, and rows of a segment up to which it has few
 // (32 tasks' rows in pieces of 128: 28.7 us instead of 24.5).
 constexpr int kPreTile = 32, kWideRows = 64;
@@ -72,9 +73,25 @@ constexpr int kSeeAll = 0x7fffffff - kMaxQueryRows;   // Piece::see of shared pa
 
 // Who plans: nobody (every sequence is one piece), every work-group, a launch before.
 enum { kWhole, kOwnPlan, kPlanned };
-// Most tokens of a table that are never cut, which saves the join: one sequence of 301
-// tokens, 8 heads of 64, 12 us instead of 19.
-constexpr int kWholeKeys = 512;
+// Whether every sequence is one piece, shared pages or not, which saves the plan and the
+// join.  By the tokens of a table (what a sequence can hold) and the groups G that this gives:
+//   up to 512: always.  1 x 301 tokens, 8 heads of 64: 19 -> 12 us; 32 sequences that
+//     share 448 tokens, 8 heads of 128: 21.4 -> 10.9; 128: 26.9 -> 27.2; 256, of 64: 33.2 -> 29.0
+//   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 20.2 -> 16.9, 32 x 8 26.4 -> 19.4,
+//     10 x 55 29.7 -> 27.3; not 8 x 8: 14.9 -> 15.5, 1 x 8: 12.4 -> 14.4; shared, from 128 to 256
+//     groups: 32 x 8 22.4 -> 15.7, 24 x 8 24.1 -> 16.6; not 64 x 8: 24.0 -> 25.7, 128 x 8: 23.4 -> 30.0
+//   up to 2048, nothing shared, where G >= 512 fills its turns of 512 groups within 1.3 times: 250 x 8 145
+//     -> 119, 200 x 8 170 -> 161, 24 x 55 98 -> 93; not 20 x 55: 93 -> 103, 10 x 55: 62 -> 69
+// Longer ones would leave one long sequence among short ones to one group.
+constexpr int kWholeKeys = 512, kWholeMore = 1024, kWholeMost = 2048, kWholeGroups = 128, kWholeShared = 256;
+
+bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles) {
+  const int64_t keys = (int64_t)c.max_pages * c.page, groups = a.batch * tiles * c.kv_heads;
+  if (keys <= kWholeKeys) return true;
+  if (keys > (shared ? kWholeMore : kWholeMost)) return false;
+  if (keys <= kWholeMore) return groups >= kWholeGroups && (!shared || groups <= kWholeShared);
+  return groups >= kHold && (groups + kHold - 1) / kHold * kHold * 10 <= groups * 13;
+}
 
 struct Space {                         // the workspace
   int32_t* count;
@@ -98,7 +115,7 @@ Limits limits(const Cache& c, const Queries& a) {
   const int64_t tiles = b * ((rows + tile - 1) / tile) + b * rows / kPreTile + b / 2;   // own rows, shared ones
   const int64_t most = (cap + kFewKeys - 1) / kFewKeys;                               // pieces of a segment
   const int64_t wide_tiles = std::min<int64_t>(b / 2, b * rows / kWideRows) + b * rows / kWide;
-  const int64_t wide_most = (cap + kWideKeys - 1) / kWideKeys;
+  const int64_t wide_most = (cap + kWideLeast - 1) / kWideLeast;
   const int64_t few = std::min<int64_t>(kGroups / kv + 1 + tiles, tiles * most);
   const int64_t wide = std::min<int64_t>(kWideGroups / kv + 1 + wide_tiles, wide_tiles * wide_most);
   return Limits{few + wide, std::min<int64_t>(kPreTile * (kGroups + kv) + 2 * kv * b * rows, 2 * kv * b * rows * most) +
@@ -248,7 +265,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  cut_keys(leads ? pre : 0, wide ? even(k1, kWideGroups, kWideKeys) : chunk, 64, pre_n, pre_l);
+  cut_keys(leads ? pre : 0, wide ? max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
   // Prefix sums: pieces of each kind, rows of results.
   const int own_all = own_n * own_tiles, pre_all = pre_n * pre_tiles;
@@ -944,11 +961,12 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
   x.a = a;
   x.sc = a.scale * kLog2e;
   x.tile = row_tile(c, a);
-  x.mode = shared == nullptr && (int64_t)c.max_pages * c.page <= kWholeKeys ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   x.rows = a.heads / c.kv_heads * a.q_len;
   x.tiles = (x.rows + x.tile - 1) / x.tile;
+  x.mode = never_cut(c, a, shared != nullptr, x.tiles) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
+  if (x.mode == kWhole) shared = nullptr;
   x.page_bits = __builtin_ctz(c.page);
-  x.narrow = (int64_t)a.batch * c.kv_heads > kHold;
+  x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;
   x.q = (const uint16_t*)q, x.kp = (const uint16_t*)kp, x.vp = (const uint16_t*)vp;
   x.tables = tables, x.lens = lens, x.ids = ids, x.shared = shared;
