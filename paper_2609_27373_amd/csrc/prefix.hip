@@ -53,13 +53,14 @@ struct Joint {
 // number of pieces, 512 / 1024 / 2048: 8 samples of 4K, 55 heads of 96, 38 / 45 /
 // 54; 128 over a 32K prefix, 8 heads of 128, 279 / 265 / 263.
 constexpr int kGroups = 1024, kFewKeys = 128, kMidKeys = 512;
-// Pieces of up to 128 rows: at most kWideGroups, one a CU beside one of few rows, and of at
-// most kWideKeys keys where that leaves kWideFill, since each leaves 128 rows of results to
-// join; of at least kWideLeast keys.  64 / 128 / 256 / 512 of them over the 32K prefix: 423 / 333
+// Pieces of up to 128 rows: at most kWideGroups / 2, one a CU beside one of few rows (two
+// where they are four times the rest: 59 instead of 62 us at 24 x 3 queries of 64 heads over
+// 12K), and of at most kWideKeys keys where that leaves kWideFill, since each leaves 128 rows
+// of results to join; of at least kWideLeast keys.  64 / 128 / 256 / 512 of them over the 32K prefix: 423 / 333
 // / 265 / 369 us; at least 256 / 512 / 768 / 1024 keys: 64.3 / 64.1 / 58.4 / 61.3 us at 64
 // sequences over 8K; filled up to 192 of them, not left at 768 keys each: 24.0 instead of 28.8 us
 // at 40 over 2K, 19.0 instead of 21.8 at 16 over 4K, 31.5 instead of 32.8 at 16 x 5 drafts over 4K.
-constexpr int kWide = 128, kWideGroups = 256, kWideFill = 192, kWideKeys = 768, kWideLeast = 256;
+constexpr int kWide = 128, kWideGroups = 512, kWideFill = 192, kWideKeys = 768, kWideLeast = 256;
 // Shared pages: rows of a piece of few rows, and rows of a segment up to which it has few
 // (32 tasks' rows in pieces of 128: 28.7 us instead of 24.5).
 constexpr int kPreTile = 32, kWideRows = 64;
@@ -265,7 +266,8 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  cut_keys(leads ? pre : 0, wide ? max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
+  const int wide_groups = k1 > 4 * k0 ? kWideGroups : kWideGroups / 2;
+  cut_keys(leads ? pre : 0, wide ? max(even(k1, wide_groups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
   // Prefix sums: pieces of each kind, rows of results.
   const int own_all = own_n * own_tiles, pre_all = pre_n * pre_tiles;
@@ -869,24 +871,30 @@ piece_kernel(Args x) {
 }
 
 // ---------------------------------------------------------------------------
-// Join: a wave a row.
+// Join: W waves a row, each its share of the pieces, eight in flight.  Four up to
+// kFewJoins rows, whose pieces are many: 7 queries of two sequences of 26K tokens, one
+// key-value head, 41 -> 20 us a call; from 1500 rows on they cost (26.4 instead of 23.9).
 // ---------------------------------------------------------------------------
-template <int D>
+constexpr int kFewJoins = 512;
+
+template <int D, int W>
 __global__ void __launch_bounds__(256)
 join_kernel(Args x, int64_t all) {
+  __shared__ float mls[4][2], part[4][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t row = W == 4 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (row >= all) return;
-  const int rows = x.rows, kv = x.c.kv_heads;
+  const int rows = x.rows, kv = x.c.kv_heads, w0 = W == 4 ? wave : 0;
   const int r = (int)(row % rows), kh = (int)(row / rows % kv), b = (int)(row / rows / kv);
   const Joint j = x.joint[b];
   if (j.done) return;
-  const int pieces = j.pre_pieces + j.own_pieces;
-  auto slot = [&](int i) {
+  const int pieces = (j.pre_pieces + j.own_pieces + W - 1 - w0) / W;   // this wave's: w0, w0 + W, ...
+  auto slot = [&](int k) {
+    const int i = w0 + W * k;
     return i < j.pre_pieces ? (size_t)j.pre_slot + ((size_t)i * kv + kh) * j.pre_rows + j.pre_row0 + r
                             : (size_t)j.own_slot + ((size_t)(i - j.pre_pieces) * kv + kh) * rows + r;
   };
-  float2 y[8];                                      // the results of eight pieces in flight
+  float2 y[8];
   auto load = [&](int i0) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
@@ -900,7 +908,7 @@ join_kernel(Args x, int64_t all) {
   for (int i = lane + 64; i < pieces; i += 64) m = fmaxf(m, x.ml[slot(i)].x);
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor(m, w, 64));
-  const float mb = m == -INFINITY ? 0.f : m;
+  float mb = m == -INFINITY ? 0.f : m;
   float l = 0.f, o0 = 0.f, o1 = 0.f;
   for (int i0 = 0; i0 < pieces; i0 += 64) {
     if (i0 > 0) ml = i0 + lane < pieces ? x.ml[slot(i0 + lane)] : float2{-INFINITY, 0.f};
@@ -921,6 +929,27 @@ join_kernel(Args x, int64_t all) {
   }
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
+  if constexpr (W == 4) {
+    if (lane < D / 2) *(float2*)(part[wave] + 2 * lane) = float2{o0, o1};
+    if (lane == 0) {
+      mls[wave][0] = m;
+      mls[wave][1] = l;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    m = fmaxf(fmaxf(mls[0][0], mls[1][0]), fmaxf(mls[2][0], mls[3][0]));
+    mb = m == -INFINITY ? 0.f : m;
+    l = o0 = o1 = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = fast_exp2(mls[w][0] - mb);
+      l += f * mls[w][1];
+      if (lane < D / 2) {
+        o0 += f * part[w][2 * lane];
+        o1 += f * part[w][2 * lane + 1];
+      }
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (lane < D / 2) *(uint32_t*)(x.o + (size_t)row * D + 2 * lane) = pack_bf16x2(o0 * inv, o1 * inv);
   if (lane == 0 && x.lse != nullptr) x.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
@@ -943,7 +972,8 @@ hipError_t launch(const Args& x, hipStream_t st) {
   else piece_kernel<D, NT, false><<<grid, 256, 0, st>>>(x);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || x.mode == kWhole) return e;
-  join_kernel<D><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(x, rows);
+  if (rows <= kFewJoins) join_kernel<D, 4><<<(unsigned)rows, 256, 0, st>>>(x, rows);
+  else join_kernel<D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(x, rows);
   return hipGetLastError();
 }
 
