@@ -55,11 +55,19 @@ class Batch:
         self.cache = PagedCache(1, pages, page, kv, d, seqs, cols, pool=pool.cuda(), tables=ints(tables.tolist()),
                                 lens=ints(all_lens.tolist()))
 
-    def run(self, shared=True, scale=0.0, out=None):
+    def roomy(self):
+        """The same cache with tables of more than 2048 tokens, which are cut and joined however few sequences hold."""
+        c = self.cache.shape
+        cols = max(c.max_pages, 2048 // c.page + 2)
+        tables = torch.full((c.seqs, cols), -1, dtype=torch.int32, device="cuda")
+        tables[:, :c.max_pages] = self.cache.tables
+        return PagedCache(1, c.pages, c.page, c.kv_heads, c.head_dim, c.seqs, cols, pool=self.cache.pool, tables=tables, lens=self.cache.lens.clone())
+
+    def run(self, shared=True, scale=0.0, out=None, cache=None):
         q = self.q.cuda()
         out = torch.full_like(q, float("nan")) if out is None else out
         lse = torch.full(q.shape[:3], float("nan"), dtype=torch.float32, device="cuda")
-        self.cache.attend(0, q, out, lse, seq_ids=ints(self.ids), shared=ints(self.shared) if shared else None, scale=scale)
+        (cache or self.cache).attend(0, q, out, lse, seq_ids=ints(self.ids), shared=ints(self.shared) if shared else None, scale=scale)
         torch.cuda.synchronize()
         return out, lse
 
@@ -76,8 +84,10 @@ class Batch:
         assert np.all(got[empty] == 0)
 
     def both(self, scale=0.0):
-        for shared in (True, False):
-            self.check(*self.run(shared, scale), scale)
+        long = bool((self.lens > self.tables.shape[1] * self.page).any())      # cut by the table itself
+        for cache in (self.cache,) if long else (self.cache, self.roomy()):
+            for shared in (True, False):
+                self.check(*self.run(shared, scale, cache=cache), scale)
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
@@ -87,7 +97,7 @@ def test_lengths(gpu_lib, page, d, gq):
     """No prefix: empty, one token, and every side of the page and tile borders."""
     tails = [None, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 300]
     b = Batch([(0, tails)], page, d, 2, gq, seed=page + d + gq)
-    b.check(*b.run(False))
+    b.both()
 
 
 @pytest.mark.parametrize("page", [16, 64, 128])
@@ -97,7 +107,7 @@ def test_lengths_beside_a_long_one(gpu_lib, page, d, gq):
     """The same where sequences are cut and joined: a table of more than 512 tokens."""
     tails = [None, 1, 16, 17, 63, 64, 65, 127, 128, 129, 256, 257, 1500, 33, None, 700]
     b = Batch([(0, tails)], page, d, 2, gq, seed=page + d + gq)
-    b.check(*b.run(False))
+    b.both()
 
 
 @pytest.mark.parametrize("batch", [63, 64, 65, 128, 200, 256, 257])
@@ -199,9 +209,12 @@ def test_scores_that_overflow(gpu_lib):
     b.pool = keep
 
 
-def test_infinite_keys_and_values(gpu_lib):
+@pytest.mark.parametrize("roomy", [False, True])
+def test_infinite_keys_and_values(gpu_lib, roomy):
     """An infinite or NaN value makes the rows that see it non-finite in its dim, and no other row or dim."""
     b = Batch([(3, [30, 40, 50, 60])], 16, 64, 2, 2, q_len=3, seed=9)
+    if roomy:
+        b.cache = b.roomy()
     ref, _ = b.run()
     p = int(b.tables[b.ids[2], 5])                    # sequence 2's newest full page, private
     pos = int(b.lens[b.ids[2]]) - 1                   # its newest token: only the last query sees it
