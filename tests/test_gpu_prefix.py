@@ -394,6 +394,50 @@ def test_long_pool(gpu_lib):
     assert torch.equal(c.pool[:, [2, 3, 0, 1]], small)
 
 
+def test_long_pool_many_rows(gpu_lib):
+    """The same for what many rows share, and for what reserve, append and its copies write there."""
+    d, kv, page, pages, n = 128, 8, 128, 20000, 24
+    c = PagedCache(1, pages, page, kv, d, n, 20, pool=torch.empty((2, pages, kv, page, d), dtype=torch.bfloat16, device="cuda"))
+    small = PagedCache(1, 64, page, kv, d, n, 20)
+    c.refs.fill_(1)
+    c.refs[-64:] = 0                                  # only the last pages are free
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((1, kv, 1000, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    k2, v2 = (torch.randn((n, kv, 2, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((n, 4 * kv, 1, d), generator=g, device="cuda").to(torch.bfloat16)
+    ids, outs = ints(list(range(n))), []
+    for x in (c, small):
+        x.append(0, k, v, ints([0]), x.reserve(ints([0]), ints([1000])))
+        assert x.fork(ints([0] * (n - 1)), ints(list(range(1, n)))).sum() == n - 1
+        x.append(0, k2, v2, ids, x.reserve(ids, ints([2] * n)))   # 24 copies of the last page
+        outs.append(x.attend(0, q, torch.empty_like(q), shared=x.shared()))
+    used = small.tables >= 0
+    assert used.sum() == 8 * n and torch.equal(c.tables[used], small.tables[used] + pages - 64)
+    assert torch.isfinite(outs[0]).all() and torch.equal(outs[0], outs[1])
+    assert torch.equal(small.shared().cpu(), torch.tensor([0] + [7] * (n - 1), dtype=torch.int32))
+
+
+def test_two_graphs_of_one_cache(gpu_lib):
+    """Two captured calls of one shape use one workspace, in turn."""
+    b = Batch([(50, [30, 5, 64, 100] * 6), (0, [900])], 16, 64, 2, 4, seed=17)
+    sh, ids = ints(b.shared), ints(b.ids)
+    qs = [b.q.cuda(), b.q.flip(0).cuda()]
+    eager = [b.cache.attend(0, q, torch.empty_like(q), seq_ids=ids, shared=s).clone() for q, s in zip(qs, (sh, None))]
+    outs, graphs = [torch.empty_like(q) for q in qs], []
+    for q, o, s in zip(qs, outs, (sh, None)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            b.cache.attend(0, q, o, seq_ids=ids, shared=s)
+    for rep in range(3):
+        for o in outs:
+            o.fill_(float("nan"))
+        for i in (0, 1) if rep % 2 else (1, 0):
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, e) for o, e in zip(outs, eager))
+        b.cache.attend(0, qs[0], torch.empty_like(qs[0]), seq_ids=ids, shared=sh)
+
+
 def test_graph_and_streams(gpu_lib):
     """Replays of a captured call between eager ones, with lengths changing; calls of two shapes on two streams."""
     b = Batch([(5, [30, 5, 64, 100] * 9), (0, [200])], 16, 128, 2, 4, seed=11)
