@@ -172,10 +172,14 @@ class PagedCache:
         return out
 
     def _attend_workspace(self, batch, heads, q_len):
-        # One per power of two of the batch, kept: a captured graph goes on using its own.
-        key = (1 << max(batch - 1, 0).bit_length(), heads, q_len)
-        if key not in self._attend:
+        # One per power of two of the batch (or the batch itself, where that many more sequences are past a
+        # limit), kept: a captured graph goes on using its own.
+        for key in ((1 << max(batch - 1, 0).bit_length(), heads, q_len), (batch, heads, q_len)):
+            if key in self._attend:
+                return self._attend[key][:2]
             n = wise.wise_prefix_workspace_bytes(self.shape, wise.make_queries(*key))
-            ws = torch.empty(max(n, 1), dtype=torch.uint8, device=self.device)
-            self._attend[key] = (ws.data_ptr(), n, ws)
-        return self._attend[key][:2]
+            if n > 0:
+                ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+                self._attend[key] = (ws.data_ptr(), n, ws)
+                return self._attend[key][:2]
+        return self._ws                         # for the call to refuse

@@ -119,6 +119,14 @@ def test_more_queries_than_indexes():
     assert wise.wise_cache_workspace_bytes(C(max_pages=1 << 25)) > 0
 
 
+def test_largest_batches_have_a_workspace():
+    c = PagedCache(1, 1, 16, 1 << 15, 64, 1024, 1, device="meta")
+    assert wise.wise_prefix_workspace_bytes(c.shape, wise.make_queries(1024, 1 << 15)) == 0     # 2^31 elements of q
+    for b in (600, 1023, 700, 600):
+        assert c._attend_workspace(b, 1 << 15, 1)[1] >= wise.wise_prefix_workspace_bytes(c.shape, wise.make_queries(b, 1 << 15)) > 0
+    assert len(c._attend) == 3                                          # kept: a captured graph goes on using its own
+
+
 def test_attention_workspace():
     a = wise.make_queries(2, 4)
     need = wise.wise_prefix_workspace_bytes(C(), a)
