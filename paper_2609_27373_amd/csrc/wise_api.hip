@@ -16,6 +16,7 @@ namespace {
 
 constexpr int64_t kI32Max = 2147483647;
 constexpr int64_t kMaxTokens = 1 << 30;       // of a sequence in a paged cache
+constexpr int64_t kMaxAppendRows = (1 << 28) - 1;   // 16 threads or fewer a row: a launch has fewer than 2^32
 constexpr int64_t kMaxPlaneHeads = 65535 * 16;   // a copy's grid has a row per 16 heads of all planes
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
@@ -356,7 +357,7 @@ wise_status wise_cache_append(const wise_cache* c, int32_t n, int32_t tokens, co
   if (n == 0) return WISE_OK;
   if ((st = check_ints({seq_ids, counts, tables, lens})) != WISE_OK) return st;
   if ((st = check_qkvo(k, v, k_pool, v_pool)) != WISE_OK) return st;
-  if ((int64_t)n * d.kv_heads > kI32Max / tokens) return WISE_ERR_SHAPE;
+  if ((int64_t)n * d.kv_heads > kMaxAppendRows / tokens) return WISE_ERR_SHAPE;
   return from_hip(wise::launch_cache_append(d, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
                                             (hipStream_t)hip_stream));
 }

@@ -92,6 +92,7 @@ def test_entries(fn):
 def test_sizes():
     assert call("append", C(), tokens=0) == SHAPE
     assert call("append", C(), n=1024, tokens=1 << 20) == SHAPE      # 2^31 rows
+    assert call("append", C(), n=1024, tokens=1 << 17) == SHAPE      # 2^28: more threads than a launch may have
     assert call("shared", C(), batch=0) == SHAPE
     assert call("shared", C(), batch=5) == SHAPE                      # 4 table rows
     assert call("shared", C(), batch=1025, ids=F) == UNSUPPORTED
