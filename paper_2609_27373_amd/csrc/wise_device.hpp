@@ -88,6 +88,14 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
+// The same, and in `rest` what the rounding left, as bf16 too: the two of a value
+// hold 16 of its bits.
+__device__ __forceinline__ uint32_t split_bf16x2(float lo, float hi, uint32_t& rest) {
+  const uint32_t w = pack_bf16x2(lo, hi);
+  rest = pack_bf16x2(lo - __builtin_bit_cast(float, w << 16), hi - __builtin_bit_cast(float, w & 0xffff0000u));
+  return w;
+}
+
 // Combine x with the value held by lane l ^ 32 (the other half of the wave
 // holding the same query column).  permlane32_swap leaves one register with
 // the low half-wave replicated and the other with the high half replicated,

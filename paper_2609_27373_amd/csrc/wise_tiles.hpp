@@ -320,13 +320,14 @@ struct WaveRows {
   // step leave nothing else to fill a wave's waits; mid(n, j) runs in slot j
   // (the copies).  The wave's priority falls through the step, so of the two
   // waves of a SIMD the one behind issues first and they reach the barrier
-  // together.  VALU and matrix cores are then both close to full.
-  template <int H, bool kQk, bool kPv, int kParts, class Mid, class Mask>
+  // together.  VALU and matrix cores are then both close to full.  kSplit: PV with 16
+  // bits of each probability, in two MFMAs a slot.
+  template <int H, bool kQk, bool kPv, int kParts, bool kSplit = false, class Mid, class Mask>
   __device__ __forceinline__ void step(const char* kn, const char* vt, const ReadAddr<D>& ra, int lane, float c,
                                        f32x16_t s[H], f32x16_t sn[H], float& mx, Mid mid, Mask maskn) {
     constexpr int kN = G::kDChunks * H;          // MFMAs of S^T; PV has as many
     constexpr int kPairs = 8 * H;
-    u32x4_t kf[kN], vf[kN], pb[2 * H];
+    u32x4_t kf[kN], vf[kN], pb[2 * H], pr[2 * H];
     auto read_k = [&](int j) {
       kf[j] = *(const u32x4_t*)(kn + ra.k[j / H] + (j % H) * 32 * Swizzle<D>::kRow);
     };
@@ -356,7 +357,15 @@ struct WaveRows {
       float& a = kParts == 0 ? ts : kParts == 4 ? tp[2 * t + (r >> 3)] : tp[t];
       a += pv[2 * k];
       a += pv[2 * k + 1];
-      uint32_t w = pack_bf16x2(pv[2 * k], pv[2 * k + 1]);
+      uint32_t w;
+      if constexpr (kSplit) {
+        uint32_t rest;
+        w = split_bf16x2(pv[2 * k], pv[2 * k + 1], rest);
+        asm volatile("" : "+v"(rest));
+        pr[2 * t + (r >> 3)][(r & 7) >> 1] = rest;
+      } else {
+        w = pack_bf16x2(pv[2 * k], pv[2 * k + 1]);
+      }
       asm volatile("" : "+v"(a), "+v"(w));
       pb[2 * t + (r >> 3)][(r & 7) >> 1] = w;
     };
@@ -425,6 +434,7 @@ struct WaveRows {
         const int i = j - kN;
         if (i + kAhead < kN) read_v(i + kAhead);
         o[i % G::kDTiles] = mfma32x32x16(vf[i], pb[i / G::kDTiles], o[i % G::kDTiles]);
+        if constexpr (kSplit) o[i % G::kDTiles] = mfma32x32x16(vf[i], pr[i / G::kDTiles], o[i % G::kDTiles]);
 #pragma unroll
         for (int k = 0; k < kPairs; ++k)
           if (k >= pairs_before(j) && k < pairs_before(j + 1)) pair_exp(k);

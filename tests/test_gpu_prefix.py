@@ -488,3 +488,28 @@ def test_after_a_prompt(gpu_lib):
     # Both are within 2^-8 |o| + 2^-8 A (rounded output, rounded probabilities) of the definition; |v| < 6 gives A < 6.
     assert (last.float() - o[:, :, -3:].float()).abs().max() <= 2 * (2 ** -8 * 6 + 2 ** -8 * 6)
     assert (z - lse[:, :, -3:]).abs().max() <= 1e-4
+
+
+@pytest.mark.parametrize("name,groups,kv,gq,q_len,cut", [
+    ("a row a sequence, whole", [(0, [1, 40, 300, 512])], 2, 4, 1, False),
+    ("a row a sequence, cut", [(0, [700, 1500, 33])], 2, 4, 1, True),
+    ("two row tiles", [(0, [700, 90])], 1, 6, 4, True),
+    ("a wave alone", [(0, [20, 64, 100, 128] * 40)], 4, 1, 1, True),
+    ("few rows share", [(12, [9, 40, 130])], 2, 4, 1, True),
+    ("many rows share", [(24, [9, 40, 130] * 8)], 2, 4, 1, True)])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_probabilities_keep_their_bits(gpu_lib, name, groups, kv, gq, q_len, cut, d):
+    """The probabilities enter the product with 16 bits: half a step of bf16 is left of each by the first part, and half
+    a step of that by the second, 2^-16 instead of the 2^-8 of the general bound."""
+    b = Batch(groups, 32, d, kv, gq, q_len, seed=d)
+    f64 = lambda t: bf16_values(t.view(torch.int16).numpy())  # noqa: E731
+    q, k, v = f64(b.q), f64(b.pool[0]), f64(b.pool[1])
+    scale = float(np.float32(1 / np.sqrt(d)))
+    o, _, bound, _ = attend(q, k, v, b.tables, b.lens, b.ids, b.page, scale)
+    rest = (bound - 2.0 ** -8 * np.abs(o)) / (1 + 2.0 ** -8)          # (2^-8 + 2 e + 2^-16) A
+    weight = attend(q, k, np.abs(v), b.tables, b.lens, b.ids, b.page, scale)[0]
+    bound = 2.0 ** -8 * np.abs(o) + (1 + 2.0 ** -8) * (rest + (2.0 ** -16 - 2.0 ** -8) * weight)
+    for shared in (True, False):
+        out, _ = b.run(shared, cache=b.roomy() if cut else None)
+        err = np.abs(out.double().cpu().numpy() - o)
+        assert np.all(err <= bound), f"{name}: {np.max(err / bound):.3g} of the bound"
