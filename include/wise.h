@@ -559,9 +559,11 @@ typedef struct {
  * all: shared[b] is the number of leading pages that sequence b shares
  * with sequence b - 1 (wise_cache_shared counts them).  shared[b] <= 0 starts a
  * run, and what a run reads once is the least shared[b] of its other sequences, at
- * most the whole pages that all queries of the run see, through the table
- * of its first sequence.  shared changes which pages are read together, and the
- * last bits, not what is computed.
+ * most the whole pages that all queries of the run see, in whole tiles of 64
+ * tokens, through the table of its first sequence.  Where neighbours share unlike
+ * numbers of pages (several prompts with a common header, a short request among
+ * users of a long prompt), runs are cut so that fewer keys are read in all.  shared
+ * changes which pages are read together, and the last bits, not what is computed.
  *
  *   q         : bf16 [batch][heads][q_len][head_dim], read-only.
  *   k_pool, v_pool : the layer's two planes, read-only.

@@ -175,10 +175,12 @@ struct Args {
 // ---------------------------------------------------------------------------
 template <int kN>
 struct Plan {                          // LDS
-  int32_t members[kN], pre_keys[kN], see[kN], first[3][kN], id[kN], len[kN], own_len[kN], own_slot[kN], pre_slot[kN],
+  int32_t members[kN], pre_keys[kN], first[3][kN], id[kN], len[kN], own_len[kN], own_slot[kN], pre_slot[kN],
       pre_pieces[kN], pre_len[kN];
   int64_t wave_keys[kN / 64][2];
   int32_t wave_sum[kN / 64][4], wave_start[kN / 64];
+  int32_t start[kN], size[kN];         // split_runs
+  unsigned long long saved[kN];
 };
 
 struct Cuts {
@@ -212,6 +214,84 @@ __device__ __forceinline__ void plan_sync() {
   }
 }
 
+// Maximum (minimum, or) of v over the planning threads; `none` changes nothing.
+template <int kN, class Op>
+__device__ __forceinline__ int plan_all(int v, int none, Op op, int32_t* waves) {
+  v = __builtin_amdgcn_readlane(wave_scan(v, none, op), 63);
+  if constexpr (kN > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = none;
+    for (int w = 0; w < kN / 64; ++w) v = op(v, waves[w]);
+  }
+  return v;
+}
+
+// Cuts runs where neighbours differ in what they share: `keys` are the keys that
+// a sequence could read together with the one before it (0: none).  A run of n that
+// reads m keys once saves (n - 1) m reads, and m is the least `keys` inside it, so one
+// pair that shares little would take the sharing from all (64 users over 8192 keys with one
+// short request among them read all 64 prompts).  From single sequences, the pairs are gone
+// through from the most keys to the fewest, an eighth at a time: runs that lie side by
+// side across pairs of at least L keys become one if each saves no less with L keys
+// a member than alone, and all together no less than apart.  On random pairs that
+// saves 99% of what the best cuts do (73% at the worst of 4000).  Pairs left after
+// kRounds go into one round.  In: s.start, s.members, s.pre_keys of single sequences.  Out:
+// the start of this sequence's run, and at a start s.members and s.pre_keys, the least `keys`.
+constexpr int kRounds = 8;
+// Bytes of K and V that cuts have to promise, up to 64 sequences and beyond, where a round has
+// barriers: the search takes 1 to 5 us, and more runs are more pieces.  us a call, uncut and
+// cut: 6 x 8 tasks of 2K with a common header, 170 MB, 35.1 and 23.8; 64 over 8K with
+// a short request among them, 220 and 48; 2 x 8 over 576, 33 MB, 18.8 and 15.7; not 8 x 5, 26 MB,
+// 18.7 and 21.6.  Beyond 64 sequences: 16 x 16 over 448, 110 MB, 34.9 and 26.8; not 16 x 5, 47 MB, 24.2
+// and 28.9, nor 40 x 2, 84 MB, 72 and 76.
+constexpr int64_t kCutBytes = 32 << 20, kCutMore = 96 << 20;
+
+template <int kN>
+__device__ __forceinline__ int split_runs(Plan<kN>& s, bool live, int keys) {
+  const int b = threadIdx.x;
+  const auto larger = [](int x, int y) { return x > y ? x : y; };
+  const auto smaller = [](int x, int y) { return x < y ? x : y; };
+  int start = b;
+  bool left = live && keys > 0;        // not gone through yet
+  for (int round = 1;; ++round) {
+    const int top = plan_all<kN>(left ? keys : 0, 0, larger, s.wave_start);
+    if (top == 0) return start;
+    const bool now = left && (round == kRounds || keys >= top - top / 8);
+    const int64_t least = plan_all<kN>(now ? keys : 0x7fffffff, 0x7fffffff, smaller, s.wave_start);
+    left = left && !now;
+    plan_sync<kN>();
+    auto joins = [&](int g) {
+      const int64_t n = s.members[g];
+      return n * least >= (n - 1) * s.pre_keys[g];
+    };
+    const bool open = now && joins(b) && joins(s.start[b - 1]);
+    int chain = wave_scan_max(start == b && !open ? b : 0);
+    if constexpr (kN > 64) {
+      if ((b & 63) == 63) s.wave_start[b >> 6] = chain;
+    }
+    s.size[b] = 0;
+    s.saved[b] = 0;
+    plan_sync<kN>();
+    for (int w = 0; w < (kN > 64 ? b >> 6 : 0); ++w) chain = max(chain, s.wave_start[w]);
+    if (live && start == b) {
+      const int n = s.members[b];
+      atomicAdd(&s.size[chain], n);
+      atomicAdd(&s.saved[chain], (unsigned long long)(n - 1) * s.pre_keys[b]);
+    }
+    plan_sync<kN>();
+    const int n = s.size[chain];
+    if ((n - 1) * least >= (int64_t)s.saved[chain]) {
+      start = chain;
+      if (b == chain) s.members[b] = n;
+      if (open) atomicMin(&s.pre_keys[chain], keys);
+    }
+    s.start[b] = start;
+    plan_sync<kN>();
+  }
+}
+
 // Runs and pieces of all sequences.  Writes x.joint if `write`.
 template <int kN>
 __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
@@ -221,27 +301,60 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
   const bool live = b < a.batch;
   const int rows = x.rows;
   const int id = !live ? -1 : x.ids ? x.ids[b] : b;
-  const int sh = live && b > 0 && x.shared ? x.shared[b] : 0;
   const int len = known_len(x, id), see = len - a.q_len + 1;
   int start = b, n = 1, pre = 0;
   if (x.shared != nullptr) {
+    // What a sequence could read together with the one before it: whole pages
+    // that every query of the two sees, in whole tiles of 64 keys (so that
+    // no piece of them needs a mask).
+    int keys = 0;
+    if (live && b > 0) {
+      const int see0 = known_len(x, x.ids ? x.ids[b - 1] : b - 1) - a.q_len + 1;
+      keys = (min(max(x.shared[b], 0), max(min(see0, see), 0) >> x.page_bits) << x.page_bits) & ~63;
+    }
     // Runs: a sequence belongs to the last start at or before it.
-    start = wave_scan_max(sh <= 0 ? b : 0);
+    start = wave_scan_max(keys == 0 ? b : 0);
     if (kN > 64 && lane == 63) s.wave_start[wave] = start;
     s.members[b] = 0;
-    s.pre_keys[b] = s.see[b] = 0x7fffffff;
+    s.pre_keys[b] = 0x7fffffff;
     plan_sync<kN>();
     for (int w = 0; w < wave; ++w) start = max(start, s.wave_start[w]);
     if (live) {
       atomicAdd(&s.members[start], 1);
-      atomicMin(&s.see[start], see);
-      if (b != start) atomicMin(&s.pre_keys[start], sh);
+      if (b != start) atomicMin(&s.pre_keys[start], keys);
     }
     plan_sync<kN>();
-    // What the run reads once: whole pages that every query sees, in whole
-    // tiles of 64 keys (so that no piece of them needs a mask).
     n = s.members[start];
-    if (n > 1) pre = (min(s.pre_keys[start], max(s.see[start], 0) >> x.page_bits) << x.page_bits) & ~63;
+    if (n > 1) pre = s.pre_keys[start];
+    // No cuts save more than the sum of `keys`: they are sought where that is an eighth more than
+    // the runs save, and kCutBytes or kCutMore of K and V more.
+    const bool inside = live && b != start;
+    int uneven = inside && keys != pre;
+    uneven = kN > 64 ? __syncthreads_or(uneven) : __builtin_amdgcn_ballot_w64(uneven) != 0;
+    if (uneven) {
+      int64_t more = wave_total(inside ? keys - pre : 0), now = wave_total(inside ? pre : 0);
+      if constexpr (kN > 64) {
+        if (lane == 0) {
+          s.wave_keys[wave][0] = more;
+          s.wave_keys[wave][1] = now;
+        }
+        __syncthreads();
+        more = now = 0;
+        for (int w = 0; w < kN / 64; ++w) {
+          more += s.wave_keys[w][0];
+          now += s.wave_keys[w][1];
+        }
+        __syncthreads();
+      }
+      if (more * 8 > now && more * c.kv_heads * c.head_dim * 4 >= (kN > 64 ? kCutMore : kCutBytes)) {
+        s.start[b] = b;
+        s.members[b] = 1;
+        s.pre_keys[b] = 0x7fffffff;
+        start = split_runs<kN>(s, live, keys);
+        n = s.members[start];
+        pre = n > 1 ? s.pre_keys[start] : 0;
+      }
+    }
   }
   const int own = len - pre, own_tiles = x.tiles;
   const bool leads = live && b == start && pre > 0;

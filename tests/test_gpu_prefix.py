@@ -513,3 +513,118 @@ def test_probabilities_keep_their_bits(gpu_lib, name, groups, kv, gq, q_len, cut
         out, _ = b.run(shared, cache=b.roomy() if cut else None)
         err = np.abs(out.double().cpu().numpy() - o)
         assert np.all(err <= bound), f"{name}: {np.max(err / bound):.3g} of the bound"
+
+
+def own_pages_gone(b, runs):
+    """b's cache in roomy tables where a run's sequences but its first name a page of NaN in place of the pages that the
+    run shares: only a call that reads these through the first one's table gives numbers.  runs: (first, end, pages)."""
+    cache = b.roomy()
+    nan = int(torch.isnan(b.pool).all(dim=4).all(dim=3).all(dim=2).all(dim=0).nonzero()[0])
+    for first, end, pages in runs:
+        for i in range(first + 1, end):
+            cache.tables[b.ids[i], :pages] = nan
+    return cache
+
+
+@pytest.mark.parametrize("border", [1, 4, 5, 20])
+@pytest.mark.parametrize("groups", [[(40, 8), (30, 9)], [(40, 20), (0, 1), (40, 33)], [(100, 30), (60, 30), (21, 30), (77, 30)],
+                                    [(30, 100)] * 3])
+def test_runs_that_share_little(gpu_lib, groups, border):
+    """Families of requests with a few common pages, or a single request among them: each family's pages are still read once."""
+    rng = random.Random(border)
+    b = Batch([(pre, [rng.randint(1, 40) for _ in range(n)]) for pre, n in groups], 32, 64, 32, 1, seed=border, slots=True)
+    runs, at = [], 0
+    for pre, n in groups:
+        runs.append((at, at + n, pre // 2 * 2))
+        at += n
+    want, _ = b.run(cache=b.roomy())
+    for first, _, _ in runs[1:]:
+        b.shared[first] = border                      # of the pages of this family and the one before
+    out, _ = b.run(cache=own_pages_gone(b, runs))
+    assert torch.isfinite(want).all() and torch.equal(out, want)
+
+
+def test_one_short_request_in_a_run(gpu_lib):
+    """A sequence of a few tokens in the middle of users of a long prompt, as shared() counts it."""
+    b = Batch([(64, [9, 30, 5] * 10), (0, [70]), (64, [9, 30, 5] * 11)], 64, 64, 2, 4, seed=19)
+    for i in range(30, 64):                           # the same first page and, but for the short one, the same prompt
+        n = 1 if i == 30 else 64
+        b.tables[b.ids[i], :n] = b.tables[b.ids[0], :n]
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    b.shared = b.cache.shared(ints(b.ids)).cpu().tolist()
+    assert b.shared == [0] + [64] * 29 + [1, 1] + [64] * 32
+    cache = b.roomy()
+    b.check(*b.run(cache=cache))
+    out, _ = b.run(cache=own_pages_gone(b, [(0, 30, 64), (31, 64, 64)]))
+    assert torch.equal(out, b.run(cache=cache)[0])
+
+
+@pytest.mark.parametrize("threads,samples,system,thread", [(8, 8, 32, 16), (3, 40, 40, 20), (40, 3, 16, 64), (2, 3, 16, 240)])
+def test_samples_of_threads(gpu_lib, threads, samples, system, thread):
+    """Samples of several threads under one system prompt: what a thread's samples share is read once for each thread where
+    that saves more than the system prompt read once for all."""
+    b = Batch([(system + thread, [1, 30, 7, 12][:samples] * (samples // min(samples, 4)))] * threads, 64, 64, 4, 1, seed=threads)
+    n = len(b.ids) // threads
+    for i in range(n, len(b.ids)):
+        b.tables[b.ids[i], :system] = b.tables[b.ids[0], :system]
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    b.shared = b.cache.shared(ints(b.ids)).cpu().tolist()
+    assert b.shared == ([0] + ([system + thread] * (n - 1) + [system]) * threads)[:len(b.ids)]
+    assert threads * (n - 1) * (system + thread) > (len(b.ids) - 1) * system
+    cache = b.roomy()
+    want, lse = b.run(cache=cache)
+    b.check(want, lse)
+    out, _ = b.run(cache=own_pages_gone(b, [(i * n, i * n + n, system + thread) for i in range(threads)]))
+    assert torch.equal(out, want)
+
+
+def test_a_little_more_is_not_worth_a_cut(gpu_lib):
+    """Pairs that share a page more than all do stay in one run, which reads what all share once."""
+    b = Batch([(40, [280, 290, 300, 270] * 9)], 64, 64, 32, 1, seed=20)
+    b.shared = [0] + [40 + 4 * (i % 2) for i in range(1, 36)]
+    for i in range(2, 36, 2):                         # 44 pages of sequence i are those of i - 1
+        b.shared[i] = 40
+    for i in range(1, 36, 2):
+        b.tables[b.ids[i], 40:44] = b.tables[b.ids[i - 1], 40:44]
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    cache = b.roomy()
+    want, lse = b.run(cache=cache)
+    b.check(want, lse)
+    assert torch.equal(b.run(cache=own_pages_gone(b, [(0, 36, 40)]))[0], want)
+
+
+class Uneven(Batch):
+    """Sequences that each share some leading pages with the one before, of any number."""
+
+    def __init__(self, batch, page, d, kv, gq, q_len, most, seed):
+        super().__init__([(0, [1])], page, d, kv, gq, q_len, seed=seed)
+        rng, g = random.Random(seed), torch.Generator().manual_seed(seed)
+        rows, lens, at = [], [], 0
+        for i in range(batch):
+            k = rng.choice((0, 1, rng.randint(0, most), most)) if rows else 0
+            row = rows[-1][:min(k, lens[-1] // page)] if rows else []
+            n = len(row) * page + rng.choice((0, 1, rng.randint(0, 2 * page), rng.randint(0, most * page - len(row) * page)))
+            new = up(n, page) - len(row)
+            rows.append(row + list(range(at, at + new)))
+            lens.append(n)
+            at += new
+        cols = max(1, max(map(len, rows)), 2048 // page + 2)
+        self.tables, self.lens, self.ids = np.full((batch, cols), -1), np.array(lens), list(range(batch))
+        for i, row in enumerate(rows):
+            self.tables[i, :len(row)] = row
+        self.pool = torch.randn((2, at + 1, kv, page, d), generator=g).to(torch.bfloat16)
+        self.q = torch.randn((batch, kv * gq, q_len, d), generator=g).to(torch.bfloat16)
+        self.cache = PagedCache(1, at + 1, page, kv, d, batch, cols, pool=self.pool.cuda(), tables=ints(self.tables.tolist()), lens=ints(lens))
+        self.shared = self.cache.shared().cpu().tolist()
+
+
+@pytest.mark.parametrize("batch,q_len,most", [(2, 1, 512), (17, 3, 4096), (64, 1, 2048), (65, 2, 4096), (256, 1, 1024), (257, 2, 1024), (600, 1, 640)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_uneven_sharing(gpu_lib, batch, q_len, most, page):
+    """Any pattern of shared pages, as shared() gives it: the definition, and the same bits at every call."""
+    for seed in range(2):
+        b = Uneven(batch, page, 64, 8, 1, q_len, most // page, seed)
+        out, lse = b.run()
+        b.check(out, lse)
+        again, lse2 = b.run()
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
