@@ -13,11 +13,12 @@ the current stream.  A serving step is
     cache.trim(ids, accepted)                   # drop drafts, or free finished ones
 
 Ids, counts and lengths are int32 tensors on the cache's device; nothing reads
-them back to the host, so a step can be captured in a HIP graph: once the buffers
-exist (a first call of attend() at each shape allocates its workspace) no call
-allocates when its output tensors are given.  Every call runs on the current
-stream of the cache's device, whichever device is current.  Graphs and streams
-that use one PagedCache share its buffers and must run in order.
+them back to the host, so a step can be captured in a HIP graph.  attend() keeps one
+workspace, which grows to the largest need seen; one that a graph has
+captured is kept for it.  No other call allocates when its output tensors
+are given.  Every call runs on the current stream of the cache's device, whichever
+device is current.  Graphs and streams that use one PagedCache share its buffers and
+must run in order.
 """
 
 from __future__ import annotations
@@ -52,11 +53,13 @@ class PagedCache:
         self._lens = self._own(lens, (seqs,), _I32, "lens", lambda s: torch.zeros(s, **i32))
         self._refs = self._own(refs, (pages,), _I32, "refs", lambda s: torch.zeros(s, **i32))
         self.device = self._pool.device
+        self._index = self.device.index
         for t, name in ((self._tables, "tables"), (self._lens, "lens"), (self._refs, "refs")):
             if t.device != self.device:
                 raise ValueError(f"{name} is on {t.device}, the pool on {self.device}")
         self._workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self._attend = {}
+        self._attend = {}                       # bytes that attend() needs, by (batch, heads, q_len)
+        self._room, self._held = None, {}       # its workspace (address, bytes, tensor); those that graphs use, by address
         # The buffers above, checked once and for all, as the C calls take them.
         self._c = ctypes.byref(self.shape)
         self._state = tuple(t.data_ptr() for t in (self._tables, self._lens, self._refs))
@@ -88,7 +91,7 @@ class PagedCache:
         return t.data_ptr()
 
     def _call(self, fn, *args):
-        index = self.device.index
+        index = self._index
         if index is None:
             raise ValueError("the cache is not on a GPU")
         entry = getattr(wise.load(), fn)
@@ -172,14 +175,30 @@ class PagedCache:
         return out
 
     def _attend_workspace(self, batch, heads, q_len):
-        # One per power of two of the batch (or the batch itself, where that many more sequences are past a
-        # limit), kept: a captured graph goes on using its own.
-        for key in ((1 << max(batch - 1, 0).bit_length(), heads, q_len), (batch, heads, q_len)):
-            if key in self._attend:
-                return self._attend[key][:2]
-            n = wise.wise_prefix_workspace_bytes(self.shape, wise.make_queries(*key))
-            if n > 0:
-                ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-                self._attend[key] = (ws.data_ptr(), n, ws)
-                return self._attend[key][:2]
-        return self._ws                         # for the call to refuse
+        key = (batch, heads, q_len)
+        n = self._attend.get(key)
+        if n is None:
+            # For a power of two of sequences, so that a growing batch grows it seldom (or for the batch itself, where
+            # that many more are past a limit).
+            sizes = ((1 << max(batch - 1, 0).bit_length(), heads, q_len), key)
+            n = next((x for x in (wise.wise_prefix_workspace_bytes(self.shape, wise.make_queries(*k)) for k in sizes) if x > 0), 0)
+            if n == 0:
+                return self._ws                 # for the call to refuse
+            self._attend[key] = n
+        capturing = self._index is not None and _stream(self._index) != 0 and self._capturing()   # the default stream can't be captured
+        if self._room is None or self._room[1] < n:
+            old, ws = self._room, torch.empty(n, dtype=torch.uint8, device=self.device)
+            self._room = (ws.data_ptr(), n, ws)
+            if old is not None and capturing:
+                self._held[old[0]] = old[2]
+            elif old is not None and ws.is_cuda:
+                # Its memory may go to others once this call's stream is here: calls of a cache run in order, so
+                # whatever used it, on any stream, has ended by then.
+                old[2].record_stream(torch.cuda.current_stream(self.device))
+        if capturing:
+            self._held[self._room[0]] = self._room[2]
+        return self._room[:2]
+
+    def _capturing(self):
+        with torch.cuda.device(self._index):
+            return torch.cuda.is_current_stream_capturing()

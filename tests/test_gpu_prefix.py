@@ -628,3 +628,81 @@ def test_uneven_sharing(gpu_lib, batch, q_len, most, page):
         b.check(out, lse)
         again, lse2 = b.run()
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_one_workspace_for_all_shapes(gpu_lib):
+    """A cache holds no more workspace than the largest of its calls needs (for the next power of two of its batch)."""
+    w = gpu_lib
+    c = PagedCache(1, 64, 64, 8, 128, 64, 128)
+    shapes = [(b, q_len) for q_len in (1, 2, 3, 4, 5) for b in (1, 3, 17, 40, 64, 20)]
+    need = max(w.wise_prefix_workspace_bytes(c.shape, w.make_queries(1 << (b - 1).bit_length(), 32, q_len)) for b, q_len in shapes)
+    q = torch.zeros((64, 32, 5, 128), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for b, q_len in shapes:
+        c.attend(0, q[:b, :, :q_len].contiguous(), out.flatten()[:b * 32 * q_len * 128].view(b, 32, q_len, 128))
+    torch.cuda.synchronize()
+    assert need <= torch.cuda.memory_allocated() - before <= need + (4 << 20)
+
+
+@pytest.mark.parametrize("eager_first", [False, True])
+def test_a_graph_keeps_its_workspace(gpu_lib, eager_first):
+    """A larger eager call after a capture, and other tensors in whatever memory it freed: replays use what they captured."""
+    b = Batch([(50, [30, 5, 64, 100]), (0, [900])], 16, 64, 2, 4, seed=21)
+    big = torch.zeros((5, 8, 16, 64), dtype=torch.bfloat16, device="cuda")
+    q, sh, ids = b.q.cuda(), ints(b.shared), ints(b.ids)
+    eager, z = (t.clone() for t in b.run(cache=Batch([(50, [30, 5, 64, 100]), (0, [900])], 16, 64, 2, 4, seed=21).cache))
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    if eager_first:
+        b.cache.attend(0, q, out, lse, seq_ids=ids, shared=sh)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.cache.attend(0, q, out, lse, seq_ids=ids, shared=sh)
+    for rep in range(3):
+        if rep == 1:
+            b.cache.attend(0, big, torch.empty_like(big), seq_ids=ids)      # grows
+        others = [torch.full((1 << 18,), float("nan"), device="cuda") for _ in range(64)]
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(lse, z)
+        assert all(torch.isnan(t).all() for t in others)
+    again = torch.cuda.CUDAGraph()                                          # one that grows it while it captures
+    big2 = torch.zeros((5, 8, 32, 64), dtype=torch.bfloat16, device="cuda")
+    out2 = torch.empty_like(big2)
+    with torch.cuda.graph(again):
+        b.cache.attend(0, big2, out2, seq_ids=ids, shared=sh)
+    want2 = b.cache.attend(0, big2, torch.empty_like(big2), seq_ids=ids, shared=sh)
+    for rep in range(2):
+        out.fill_(float("nan"))
+        out2.fill_(float("nan"))
+        again.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(out2, want2)
+
+
+def test_a_workspace_outgrown_on_another_stream(gpu_lib):
+    """Calls in order on two streams, the second of which outgrows the workspace: its memory goes to nobody before the first is done."""
+    b = Batch([(200, [30, 5, 64, 100] * 8)], 16, 64, 8, 4, seed=22)
+    q, ids = b.q.cuda(), ints(b.ids)
+    big = torch.zeros((32, 32, 8, 64), dtype=torch.bfloat16, device="cuda")
+    want = b.run(shared=False)[0].clone()
+    for rep in range(3):
+        c = PagedCache(1, b.cache.shape.pages, 16, 8, 64, b.cache.shape.seqs, b.cache.shape.max_pages, pool=b.cache.pool, tables=b.cache.tables,
+                       lens=b.cache.lens)
+        s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+        outs, out2 = [torch.empty_like(q) for _ in range(20)], torch.empty_like(big)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s1):
+            for o in outs:
+                c.attend(0, q, o, seq_ids=ids)
+        s2.wait_stream(s1)
+        with torch.cuda.stream(s2):
+            c.attend(0, big, out2, seq_ids=ids)
+        with torch.cuda.stream(s1):
+            torch.full((1 << 24,), float("nan"), device="cuda")
+        torch.full((1 << 24,), float("nan"), device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs)
