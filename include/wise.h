@@ -495,7 +495,7 @@ wise_status wise_cache_reserve(const wise_cache* c, int32_t n,
  *             counts[i] on are not read.
  *   k_pool, v_pool : the layer's two planes, [pages][kv_heads][page][head_dim].
  * Errors: as wise_cache_fork (WISE_ERR_SHAPE also for tokens < 1 and for
- *         n * kv_heads * tokens >= 2^28).
+ *         n * kv_heads * tokens > 2^28 - 16).
  */
 wise_status wise_cache_append(const wise_cache* c, int32_t n, int32_t tokens,
                               const int32_t* seq_ids, const int32_t* counts,

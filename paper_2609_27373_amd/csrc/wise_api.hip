@@ -16,7 +16,7 @@ namespace {
 
 constexpr int64_t kI32Max = 2147483647;
 constexpr int64_t kMaxTokens = 1 << 30;       // of a sequence in a paged cache
-constexpr int64_t kMaxAppendRows = (1 << 28) - 1;   // 16 threads or fewer a row: a launch has fewer than 2^32
+constexpr int64_t kMaxAppendRows = (1 << 28) - 16;   // groups of 256 threads on 16 rows or more: a launch has fewer than 2^32 threads
 constexpr int64_t kMaxPlaneHeads = 65535 * 16;   // a copy's grid has a row per 16 heads of all planes
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }

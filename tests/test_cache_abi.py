@@ -182,3 +182,16 @@ def test_model_by_hand():
     assert m.tables[1] == [0, 1, -1] and m.refs == [2, 1, 1, 1, 0, 0] and m.counts_hold()
     m.trim([2, 0], [4, 0])
     assert m.tables[2] == [0, -1, -1] and m.lens == [0, 6, 4, 0] and m.counts_hold()
+
+
+def test_append_rows_that_one_launch_holds():
+    """2^28 - 1 and 2^28 - 15 rows round up to 2^24 groups of 256 threads at head_dim 128: 2^32, more than a launch may have."""
+    for d in (64, 96, 128):
+        assert 381 * 43 * 16385 == (1 << 28) - 1
+        assert call("append", C(kv_heads=16385, page=16, head_dim=d), n=381, tokens=43) == SHAPE
+        assert call("append", C(kv_heads=1, head_dim=d), n=1, tokens=(1 << 28) - 15) == SHAPE
+        # The largest that is accepted, by both kernels: rows a group when tokens are few; tiles of 32 or 64 tokens.
+        rows = (1 << 28) - 16
+        few = -(-rows // (256 // (d // 8))) * 256
+        many = max(-(-rows // t) * -(-t // (64 if d == 96 else 32)) * 256 for t in range(64, 4096))
+        assert few < 1 << 32 and many < 1 << 32
