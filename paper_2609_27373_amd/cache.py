@@ -18,7 +18,7 @@ workspace, which grows to the largest need seen; one that a graph has
 captured is kept for it.  No other call allocates when its output tensors
 are given.  Every call runs on the current stream of the cache's device, whichever
 device is current.  Graphs and streams that use one PagedCache share its buffers and
-must run in order.
+must run in order.  A call on no sequences at all does nothing.
 """
 
 from __future__ import annotations
@@ -132,8 +132,10 @@ class PagedCache:
             raise ValueError(f"k and v must be [{n}][{c.kv_heads}][tokens][{c.head_dim}], got {tuple(k.shape)}, {tuple(v.shape)}")
         kp, vp = self._layer(layer)
         rows = k.numel()
-        self._call("wise_cache_append", n, k.shape[2], self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n),
-                   self._arg(k, _BF16, "k", rows), self._arg(v, _BF16, "v", rows), *self._state[:2], kp, vp)
+        args = (self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n), self._arg(k, _BF16, "k", rows),
+                self._arg(v, _BF16, "v", rows))
+        if n > 0:
+            self._call("wise_cache_append", n, k.shape[2], *args, *self._state[:2], kp, vp)
 
     def _layer(self, layer):
         if not 0 <= layer < self.shape.planes // 2:
@@ -157,8 +159,9 @@ class PagedCache:
         """Leading pages that each sequence has in common with the one before it (all sequences without seq_ids)."""
         batch = self.shape.seqs if seq_ids is None else seq_ids.numel()
         out = self._ints(batch) if out is None else out
-        self._call("wise_cache_shared", batch, min_pages, self._arg(seq_ids, _I32, "seq_ids", batch), *self._state[:2],
-                   self._arg(out, _I32, "out", batch))
+        args = self._arg(seq_ids, _I32, "seq_ids", batch), *self._state[:2], self._arg(out, _I32, "out", batch)
+        if batch > 0:
+            self._call("wise_cache_shared", batch, min_pages, *args)
         return out
 
     def attend(self, layer, q, out, lse=None, seq_ids=None, shared=None, scale=0.0):
@@ -169,9 +172,11 @@ class PagedCache:
         batch, heads, q_len = q.shape[:3]
         kp, vp = self._layer(layer)
         n, rows = q.numel(), batch * heads * q_len
-        self._call("wise_prefix_attn", ctypes.byref(wise.wise_queries(batch, heads, q_len, scale)), self._arg(q, _BF16, "q", n), kp, vp,
-                   *self._state[:2], self._arg(seq_ids, _I32, "seq_ids", batch), self._arg(shared, _I32, "shared", batch),
-                   self._arg(out, _BF16, "out", n), self._arg(lse, _F32, "lse", rows), *self._attend_workspace(batch, heads, q_len))
+        args = (self._arg(q, _BF16, "q", n), kp, vp, *self._state[:2], self._arg(seq_ids, _I32, "seq_ids", batch),
+                self._arg(shared, _I32, "shared", batch), self._arg(out, _BF16, "out", n), self._arg(lse, _F32, "lse", rows))
+        if batch > 0:
+            self._call("wise_prefix_attn", ctypes.byref(wise.wise_queries(batch, heads, q_len, scale)), *args,
+                       *self._attend_workspace(batch, heads, q_len))
         return out
 
     def _attend_workspace(self, batch, heads, q_len):

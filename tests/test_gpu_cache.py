@@ -358,3 +358,24 @@ def test_paged_cache_arguments(gpu_lib):
     with pytest.raises(gpu_lib.WiseError):
         c.trim(torch.zeros(1025, dtype=torch.int32, device="cuda"))
     same(c, m)
+
+
+def test_a_step_with_nothing_to_do(gpu_lib):
+    """Every call of a serving step takes an empty batch, still checks its arguments, and changes nothing."""
+    c, m = pair()
+    grow(c, m, [0], [20])
+    none = ints([])
+    k = torch.empty((0, 2, 0, 64), dtype=torch.bfloat16, device="cuda")
+    q = torch.empty((0, 4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    c.trim(none, none)
+    assert c.fork(none, none).numel() == 0 and c.reserve(none, none).numel() == 0
+    c.append(0, k, k, none, none)
+    shared = c.shared(none)
+    assert shared.shape == (0,) and shared.dtype == torch.int32
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    assert c.attend(0, q, out, lse, seq_ids=none, shared=shared) is out
+    same(c, m)
+    for call in (lambda: c.shared(torch.empty(0, device="cuda")), lambda: c.attend(0, q, out.float()), lambda: c.attend(1, q, out),
+                 lambda: c.append(0, k.half(), k.half(), none, none), lambda: c.append(1, k, k, none, none)):
+        with pytest.raises(ValueError):
+            call()
