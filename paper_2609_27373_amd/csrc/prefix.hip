@@ -80,8 +80,10 @@ constexpr int kSeeAll = 0x7fffffff - kMaxQueryRows;   // Piece::see of shared pa
 enum { kWhole, kOwnPlan, kPlanned };
 // Whether every sequence is one piece, shared pages or not, which saves the plan and the
 // join.  By the tokens of a table (what a sequence can hold) and the groups G that this gives:
-//   up to 512: always.  1 x 301 tokens, 8 heads of 64: 19 -> 12 us; 32 sequences that
-//     share 448 tokens, 8 heads of 128: 21.4 -> 10.9; 128: 26.9 -> 27.2; 256, of 64: 33.2 -> 29.0
+//   up to 512: always, nothing shared.  1 x 301 tokens, 8 heads of 64: 12 -> 7.5 us; 1024 sequences of
+//     512 tokens, 8 heads of 128: 194 -> 161.  Where they share 448 tokens, while the whole tables
+//     are 256 MB of K and V: 64 x 8 heads of 128 17.2 -> 15.3, 256 x 8 of 64 28.2 -> 27.4; at the limit 128 x 8
+//     of 128 21.0 -> 24.5 but 30.2 -> 25.4 at 256 x 8, 256 tokens; not 512 x 8 of 64: 36 -> 50, 1024 x 8 of 128: 66 -> 160
 //   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 20.2 -> 16.9, 32 x 8 26.4 -> 19.4,
 //     10 x 55 29.7 -> 27.3; not 8 x 8: 14.9 -> 15.5, 1 x 8: 12.4 -> 14.4; shared, from 128 to 256
 //     groups: 32 x 8 22.4 -> 15.7, 24 x 8 24.1 -> 16.6; not 64 x 8: 24.0 -> 25.7, 128 x 8: 23.4 -> 30.0
@@ -89,10 +91,11 @@ enum { kWhole, kOwnPlan, kPlanned };
 //     -> 119, 200 x 8 170 -> 161, 24 x 55 98 -> 93; not 20 x 55: 93 -> 103, 10 x 55: 62 -> 69
 // Longer ones would leave one long sequence among short ones to one group.
 constexpr int kWholeKeys = 512, kWholeMore = 1024, kWholeMost = 2048, kWholeGroups = 128, kWholeShared = 256;
+constexpr int64_t kWholeBytes = 256 << 20;
 
 bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles) {
   const int64_t keys = (int64_t)c.max_pages * c.page, groups = a.batch * tiles * c.kv_heads;
-  if (keys <= kWholeKeys) return true;
+  if (keys <= kWholeKeys) return !shared || groups * keys * c.head_dim * 4 <= kWholeBytes;
   if (keys > (shared ? kWholeMore : kWholeMost)) return false;
   if (keys <= kWholeMore) return groups >= kWholeGroups && (!shared || groups <= kWholeShared);
   return groups >= kHold && (groups + kHold - 1) / kHold * kHold * 10 <= groups * 13;

@@ -706,3 +706,17 @@ def test_a_workspace_outgrown_on_another_stream(gpu_lib):
         torch.full((1 << 24,), float("nan"), device="cuda")
         torch.cuda.synchronize()
         assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("d,kv,gq,batch", [(128, 8, 1, 150), (64, 8, 2, 300), (96, 16, 1, 100), (64, 1, 8, 1024)])
+def test_many_sequences_of_short_tables(gpu_lib, d, kv, gq, batch):
+    """Tables of 512 tokens whose K and V, all read for themselves, would be more than 256 MB: what they share is read once."""
+    b = Batch([(14, [1 + 5 * i % 64 for i in range(batch)])], 32, d, kv, gq, seed=d + kv)
+    assert b.cache.shape.max_pages * 32 == 512
+    b.check(*b.run())
+    b.check(*b.run(shared=False))
+    if batch * kv * 512 * d * 4 > 256 << 20:
+        want = b.run()[0].clone()
+        nan = int(torch.isnan(b.pool).all(dim=4).all(dim=3).all(dim=2).all(dim=0).nonzero()[0])
+        b.cache.tables[1:batch, :14] = nan
+        assert torch.isfinite(want).all() and torch.equal(b.run()[0], want)
