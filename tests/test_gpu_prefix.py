@@ -720,3 +720,38 @@ def test_many_sequences_of_short_tables(gpu_lib, d, kv, gq, batch):
         nan = int(torch.isnan(b.pool).all(dim=4).all(dim=3).all(dim=2).all(dim=0).nonzero()[0])
         b.cache.tables[1:batch, :14] = nan
         assert torch.isfinite(want).all() and torch.equal(b.run()[0], want)
+
+
+def test_after_a_prompt_element_by_element(gpu_lib):
+    """The prompt's K and V go into the cache by append, and its last tokens attend as in the dense call: both are held, element by
+    element, to the definition computed from the prompt itself, closely enough that one value in the wrong place shows."""
+    w = gpu_lib
+    n, heads, kv, d, q_len = 320, 8, 2, 96, 3
+    g = torch.Generator(device="cuda").manual_seed(23)
+    q, k, v = (torch.randn((2, h, n, d), generator=g, device="cuda").to(torch.bfloat16) for h in (heads, kv, kv))
+    dense = torch.empty_like(q)
+    w.wise_dense_attn_accum(w.make_shape(2, heads, n, d, 64, kv_heads=kv), q, k, v, dense)
+    c = PagedCache(1, 30, 32, kv, d, 4, 12)
+    ids = ints([2, 0])
+    c.append(0, k, v, ids, c.reserve(ids, ints([n, n])))
+    out, lse = torch.empty((2, heads, q_len, d), dtype=torch.bfloat16, device="cuda"), torch.empty((2, heads, q_len), device="cuda")
+    c.attend(0, q[:, :, -q_len:].contiguous(), out, lse, seq_ids=ids)
+    gq, seen = heads // kv, set()
+    for b in range(2):
+        for h in range(heads):
+            for t in range(q_len):
+                see = n - q_len + 1 + t
+                row, keys, values = q[b, h, see - 1][None], k[b, h // gq, :see], v[b, h // gq, :see]
+                o, z, bound, zb = reference_on_gpu(row, keys, values)
+                # the cache's probabilities have 16 bits in the product, the dense kernel's 8
+                weight = reference_on_gpu(row, keys, values.abs())[0]
+                close = bound + (1 + 2.0 ** -8) * (2.0 ** -16 - 2.0 ** -8) * weight
+                assert ((out[b, h, t].double() - o[0]).abs() <= close[0]).all()
+                assert ((lse[b, h, t].double() - z[0]).abs() <= zb[0])
+                assert ((dense[b, h, see - 1].double() - o[0]).abs() <= bound[0]).all()
+                # the newest token's values missing, or those of two tokens exchanged, would be seen
+                for i, wrong in enumerate((torch.cat([values[:-1], torch.zeros_like(values[:1])]), values[[1, 0] + list(range(2, see))])):
+                    off = reference_on_gpu(row, keys, wrong)[0]
+                    if ((out[b, h, t].double() - off[0]).abs() > close[0]).any():
+                        seen.add((i, b, h // gq))
+    assert len(seen) == 2 * 2 * kv                    # by some row of every key-value head
