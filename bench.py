@@ -12,7 +12,8 @@ FLOPs per admitted causal (query, key) pair of the selected support), with
 its fraction of the bf16 dense MFMA peak, the speedup over this library's own
 dense kernel on the same late-step inputs, and the paper-regime variant of
 the same workload beside it.  Further legs, each with its own manifest
-(seed, SHA-256 of the first and last step's inputs and of the CSR): the
+(seed, SHA-256 of the first and last step's inputs and of the CSR; in the
+leg's full record, a line on stderr): the
 paper's geometry (4K, 220 heads, d 96, 32-key blocks) under both selection
 rules, with the same sparse kernel on the full causal support beside the
 selected one (the paper's matched-backend comparison); the paper's
@@ -385,8 +386,16 @@ def cpu_baseline(cfg, min_s=10.0, max_late=8):
                       f"host {os.cpu_count()} logical CPUs"}
 
 
+# What the JSON line says of a leg; everything else of it, the manifest among it,
+# is in the leg's own line on stderr.  With all of it the line was longer than the
+# 16,000 characters that a record of the output keeps.
+LINE_KEYS = ("workload", "mode", "tau", "late_kernel", "density", "late_ms", "late_tflops", "dense_ms", "dense_tflops",
+             "select_ms", "discovery_ms", "speedup_prepared", "speedup_trajectory", "speedup_matched_backend",
+             "retained_future_mass_mean", "j_roll_mean_late")
+
+
 def rounded(r):
-    return {k: (round(v, 5) if isinstance(v, float) else v) for k, v in r.items()}
+    return {k: (round(r[k], 5) if isinstance(r[k], float) else r[k]) for k in LINE_KEYS if k in r}
 
 
 def main():
