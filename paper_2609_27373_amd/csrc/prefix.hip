@@ -54,24 +54,25 @@ struct Joint {
 // Sizes of the pieces.  Pieces of few rows: so many that there are kGroups / 2
 // (the work-groups that the chip holds at once), of at least kFewKeys keys; where
 // that makes them longer than kMidKeys, so many that there are kGroups.  us a call by the
-// number of pieces, 512 / 1024 / 2048: 8 samples of 4K, 55 heads of 96, 38 / 45 /
-// 54; 128 over a 32K prefix, 8 heads of 128, 279 / 265 / 263.
+// number of pieces, 512 / 1024 / 2048: 8 samples of 4K, 55 heads of 96, 31.9 / 32.1 /
+// 36.3; 128 over a 32K prefix, 8 heads of 128, 289 / 256 / 303.
 constexpr int kGroups = 1024, kFewKeys = 128, kMidKeys = 512;
-// Pieces of up to 128 rows: at most kWideGroups / 2, one a CU beside one of few rows (two
-// where they are four times the rest: 59 instead of 62 us at 24 x 3 queries of 64 heads over
-// 12K), and of at most kWideKeys keys where that leaves kWideFill, since each leaves 128 rows
-// of results to join; of at least kWideLeast keys.  64 / 128 / 256 / 512 of them over the 32K prefix: 423 / 333
-// / 265 / 369 us; at least 256 / 512 / 768 / 1024 keys: 64.3 / 64.1 / 58.4 / 61.3 us at 64
-// sequences over 8K; filled up to 192 of them, not left at 768 keys each: 24.0 instead of 28.8 us
-// at 40 over 2K, 19.0 instead of 21.8 at 16 over 4K, 31.5 instead of 32.8 at 16 x 5 drafts over 4K.
-constexpr int kWide = 128, kWideGroups = 512, kWideFill = 192, kWideKeys = 768, kWideLeast = 256;
+// Pieces of up to 128 rows: at most kWideGroups, one a CU beside one of few rows (two, where
+// those are few, are as often worse as better: 57 instead of 53 us at 128 over 32K with tails of 16, but 75
+// instead of 80 over 30K under 4 heads of 64), and of at most kWideKeys keys where that leaves kWideFill, since each leaves 128 rows
+// of results to join; of at least kWideLeast keys.  64 / 128 / 256 / 512 of them over the 32K prefix: 482 / 320
+// / 256 / 331 us; at most 256 / 512 / 768 / 1024 keys: 58.0 / 58.3 / 53.1 / 53.3 us at 64
+// sequences over 8K; filled up to 192 of them, not left at 768 keys each: 23.3 instead of 31.2 us
+// at 40 over 2K, 32.5 instead of 34.9 at 16 x 5 drafts over 4K.
+constexpr int kWide = 128, kWideGroups = 256, kWideFill = 192, kWideKeys = 768, kWideLeast = 256;
 // Shared pages: rows of a piece of few rows, and rows of a segment up to which it has few
-// (32 tasks' rows in pieces of 128: 28.7 us instead of 24.5).
+// (3 x 12 requests' 48 rows over 8K in a piece of 128: 43.8 us instead of 41.1; 120 rows over 16K in
+// pieces of 32: 50 instead of 36).
 constexpr int kPreTile = 32, kWideRows = 64;
 // Where there are more (sequence, head)s than groups: keys of a sequence's own up to
 // which a wave takes them alone, four heads a group, since the latency of a piece is most of
-// its time (128 sequences of up to 64 tokens over a 16K prefix, 16 heads of 64: 40 us
-// instead of 49).
+// its time (128 sequences of up to 64 tokens over a 16K prefix, 64 heads of 64 on 16: 92 us
+// instead of 103).
 constexpr int kNarrowKeys = 128, kHold = 512;
 
 constexpr int kSeeAll = 0x7fffffff - kMaxQueryRows;   // Piece::see of shared pages
@@ -84,11 +85,12 @@ enum { kWhole, kOwnPlan, kPlanned };
 //     512 tokens, 8 heads of 128: 194 -> 161.  Where they share 448 tokens, while the whole tables
 //     are 256 MB of K and V: 64 x 8 heads of 128 17.2 -> 15.3, 256 x 8 of 64 28.2 -> 27.4; at the limit 128 x 8
 //     of 128 21.0 -> 24.5 but 30.2 -> 25.4 at 256 x 8, 256 tokens; not 512 x 8 of 64: 36 -> 50, 1024 x 8 of 128: 66 -> 160
-//   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 20.2 -> 16.9, 32 x 8 26.4 -> 19.4,
-//     10 x 55 29.7 -> 27.3; not 8 x 8: 14.9 -> 15.5, 1 x 8: 12.4 -> 14.4; shared, from 128 to 256
-//     groups: 32 x 8 22.4 -> 15.7, 24 x 8 24.1 -> 16.6; not 64 x 8: 24.0 -> 25.7, 128 x 8: 23.4 -> 30.0
-//   up to 2048, nothing shared, where G >= 512 fills its turns of 512 groups within 1.3 times: 250 x 8 145
-//     -> 119, 200 x 8 170 -> 161, 24 x 55 98 -> 93; not 20 x 55: 93 -> 103, 10 x 55: 62 -> 69
+//   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 21.4 -> 16.5, 32 x 8 24.7 -> 18.3 (10 x 55
+//     32.9 -> 33.8); not 8 x 8: 15.1 -> 16.3, 1 x 8: 11.7 -> 14.2; shared, from 128 to 256
+//     groups: 32 x 8 21.2 -> 16.2, 24 x 8 20.2 -> 15.6; not 64 x 8: 25.0 -> 25.4, 128 x 8: 34.0 -> 43.1
+//   up to 2048, nothing shared, where G >= 512 fills its turns of 512 groups within 1.3 times: 250 x 8 117
+//     -> 100, 200 x 8 181 -> 152, 24 x 55 114 -> 101; past 1.3 either may win: 20 x 55 92 -> 83, 131 x 8 105
+//     -> 118; 10 x 55, 1.86: 59 -> 65
 // Longer ones would leave one long sequence among short ones to one group.
 constexpr int kWholeKeys = 512, kWholeMore = 1024, kWholeMost = 2048, kWholeGroups = 128, kWholeShared = 256;
 constexpr int64_t kWholeBytes = 256 << 20;
@@ -193,7 +195,7 @@ struct Cuts {
 __device__ __forceinline__ int up_to(int x, int y) { return (int)(((uint32_t)x + y - 1) / (uint32_t)y); }
 
 // Pieces of `keys` keys when a piece should hold about `chunk`, and their even length
-// (pieces of `chunk` and a rest: 265 us instead of 254 at 128 sequences over 32K).
+// (pieces of `chunk` and a rest: 263 us instead of 256 at 128 sequences over 32K).
 __device__ __forceinline__ void cut_keys(int keys, int chunk, int unit, int& pieces, int& len) {
   pieces = 0;
   len = unit;
@@ -386,8 +388,7 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  const int wide_groups = k1 > 4 * k0 ? kWideGroups : kWideGroups / 2;
-  cut_keys(leads ? pre : 0, wide ? max(even(k1, wide_groups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
+  cut_keys(leads ? pre : 0, wide ? max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
   // Prefix sums: pieces of each kind, rows of results.
   const int own_all = own_n * own_tiles, pre_all = pre_n * pre_tiles;
@@ -576,8 +577,8 @@ template <>
 struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(16))); };
 
 // threadIdx.x, unknown to the compiler: what a piece computes from it would else be
-// kept in registers over the loop over pieces, for every kind of piece at once (56
-// registers spilled at D = 128, 66 us instead of 54 at 64 sequences over 8K).
+// kept in registers over the loop over pieces, for every kind of piece at once
+// (registers spilled at D = 128, 60 us instead of 53 at 64 sequences over 8K).
 __device__ __forceinline__ int fresh_tid() {
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
@@ -833,7 +834,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 // 64): the software pipeline of the dense kernel (WaveRows::step), four waves
 // of 32 rows over rings of two K and two V tiles in LDS.  A wave copies 16
 // consecutive keys of a tile, which lie in one page.  Bound by the matrix
-// cores and the exponentials, 1.3 us a tile of 64 keys of 128 beside a group of few
+// cores and the exponentials, 1.5 us a tile of 64 keys of 128 beside a group of few
 // rows.  False, with nothing done, if some page id of the piece names no page.
 // ---------------------------------------------------------------------------
 template <int D>
@@ -996,7 +997,7 @@ piece_kernel(Args x) {
 // ---------------------------------------------------------------------------
 // Join: W waves a row, each its share of the pieces, eight in flight.  Four up to
 // kFewJoins rows, whose pieces are many: 7 queries of two sequences of 26K tokens, one
-// key-value head, 41 -> 20 us a call; from 1500 rows on they cost (26.4 instead of 23.9).
+// key-value head, 40 -> 21 us a call; from 1500 rows on they cost (47.5 instead of 45.3).
 // ---------------------------------------------------------------------------
 constexpr int kFewJoins = 512;
 
@@ -1087,7 +1088,7 @@ hipError_t launch(const Args& x, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   // Two groups a CU (registers allow few kinds more, and three or four do worse where
-  // they do: 63 and 64 us instead of 58 at 32 sequences of up to 4K), or as many as do
+  // they do: 62 and 64 us instead of 58 at 32 sequences of up to 4K), or as many as do
   // all the pieces kTodo at a time.
   const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = kHold;
   const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
