@@ -575,6 +575,8 @@ typedef struct {
  *   shared    : int32 [batch], device, or NULL: nothing is shared.
  *   o         : bf16 [batch][heads][q_len][head_dim], written.  A row that sees
  *               no position is zero (and its lse -inf).
+ *               An infinite value is what its dim of a row that sees it gets, whatever its
+ *               weight (NaN beside NaN or the other infinity), and no other row or dim.
  *   lse       : fp32 [batch][heads][q_len] or NULL: natural log of the sum.
  *   workspace : device scratch of wise_prefix_workspace_bytes(c, a) bytes, 256-byte
  *               aligned; contents on entry are ignored.

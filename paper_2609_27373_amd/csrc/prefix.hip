@@ -576,6 +576,28 @@ struct VRow<96> { typedef uint32_t type __attribute__((ext_vector_type(3), align
 template <>
 struct VRow<128> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(16))); };
 
+// Puts into o, dims d .. d + 3 of a row's values, the sum of the infinite and NaN values
+// of keys k0 .. end - 1 where there are any: what a row that sees them gets, whatever
+// their weights.  The product makes NaN of an infinite value whose weight, or the second
+// part of it, is 0 or of the other sign, and leaves out those of tiles with a mask.
+template <int D>
+__device__ __forceinline__ void put_unbounded(const Args& x, const int32_t* table, int kh, int k0, int end, int d, f32x4_t& o) {
+  f32x4_t sum{};
+#pragma unroll 1
+  for (int key = k0; key < end; ++key) {
+    const int id = table[key >> x.page_bits];
+    if (!in_range(id, x.c.pages)) continue;
+    const uint16_t* v = x.vp + (((size_t)id * x.c.kv_heads + kh) * x.c.page + (key & (x.c.page - 1))) * D + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((v[i] & 0x7f80) == 0x7f80) sum[i] += __builtin_bit_cast(float, (uint32_t)v[i] << 16);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (sum[i] != 0.f) o[i] = sum[i];
+}
+__device__ __forceinline__ bool any_nan(const f32x4_t& o) { return o[0] != o[0] || o[1] != o[1] || o[2] != o[2] || o[3] != o[3]; }
+
 // threadIdx.x, unknown to the compiler: what a piece computes from it would else be
 // kept in registers over the loop over pieces, for every kind of piece at once
 // (registers spilled at D = 128, 60 us instead of 53 at 64 sequences over 8K).
@@ -805,17 +827,8 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       lt += f * mls[2 * (w * kRows + r) + 1];
       sum += f * *(const f32x4_t*)(lds + (w * kRows + r) * kStride + d);
     }
-    if (poisoned) {                                 // infinite and NaN values of the keys that row r sees
-      const int end = min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1);
-      for (int key = p.k0; key < end; ++key) {
-        const int id = table[key >> x.page_bits];
-        if (!in_range(id, x.c.pages)) continue;
-        const uint16_t* v = x.vp + (((size_t)id * x.c.kv_heads + kh) * page + (key & (page - 1))) * D + d;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((v[i] & 0x7f80) == 0x7f80) sum[i] += __builtin_bit_cast(float, (uint32_t)v[i] << 16);
-      }
-    }
+    if (poisoned || (lt == lt && any_nan(sum)))
+      put_unbounded<D>(x, table, kh, p.k0, min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1), d, sum);
     if (p.slot >= 0) {
       const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + r;
       *(f32x4_t*)(x.part + at * D + d) = sum;
@@ -956,6 +969,20 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
       *(f32x4_t*)(x.part + at * D + 32 * t + 8 * j + 4 * h) =
           f32x4_t{w.o[t][4 * j], w.o[t][4 * j + 1], w.o[t][4 * j + 2], w.o[t][4 * j + 3]};
   if (h == 0) x.ml[at] = float2{w.m, lt};
+  float all = 0.f;
+#pragma unroll
+  for (int t = 0; t < G::kDTiles; ++t)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) all += w.o[t][j];
+  if (lt == lt && all != all) {                     // of infinite values
+#pragma unroll 1
+    for (int d = 4 * h; d < D; d += 8) {
+      f32x4_t o = *(const f32x4_t*)(x.part + at * D + d);
+      if (!any_nan(o)) continue;
+      put_unbounded<D>(x, table, kh, p.k0, p.k1, d, o);
+      *(f32x4_t*)(x.part + at * D + d) = o;
+    }
+  }
   return true;
 }
 
@@ -1053,6 +1080,19 @@ join_kernel(Args x, int64_t all) {
   }
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
+  // An infinite part counts whatever its weight, and 0 times it is NaN.
+  auto unbounded = [](float& u, float y) { u += __builtin_isfinite(y) ? 0.f : y; };
+  if (l == l && (o0 != o0 || o1 != o1)) {
+    float u0 = 0.f, u1 = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < pieces; ++i) {
+      const float2 z = *(const float2*)(x.part + slot(i) * D + 2 * lane);
+      unbounded(u0, z.x);
+      unbounded(u1, z.y);
+    }
+    if (u0 != 0.f) o0 = u0;
+    if (u1 != 0.f) o1 = u1;
+  }
   if constexpr (W == 4) {
     if (lane < D / 2) *(float2*)(part[wave] + 2 * lane) = float2{o0, o1};
     if (lane == 0) {
@@ -1072,6 +1112,16 @@ join_kernel(Args x, int64_t all) {
         o0 += f * part[w][2 * lane];
         o1 += f * part[w][2 * lane + 1];
       }
+    }
+    if (l == l && (o0 != o0 || o1 != o1)) {
+      float u0 = 0.f, u1 = 0.f;
+#pragma unroll 1
+      for (int w = 0; w < 4; ++w) {
+        unbounded(u0, part[w][2 * lane]);
+        unbounded(u1, part[w][2 * lane + 1]);
+      }
+      if (u0 != 0.f) o0 = u0;
+      if (u1 != 0.f) o1 = u1;
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;

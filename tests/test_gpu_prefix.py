@@ -755,3 +755,33 @@ def test_after_a_prompt_element_by_element(gpu_lib):
                     if ((out[b, h, t].double() - off[0]).abs() > close[0]).any():
                         seen.add((i, b, h // gq))
     assert len(seen) == 2 * 2 * kv                    # by some row of every key-value head
+
+
+@pytest.mark.parametrize("name,groups,kv,gq,q_len,cut", [
+    ("a row a sequence, whole", [(4, [40, 300, 200])], 2, 4, 1, False),
+    ("a row a sequence, cut", [(4, [700, 1500, 33])], 2, 4, 1, True),
+    ("two row tiles", [(4, [700, 90])], 1, 6, 4, True),
+    ("a wave alone", [(2, [20, 40, 61] * 54)], 4, 1, 1, True),
+    ("few rows share", [(12, [9, 40, 130])], 2, 4, 1, True),
+    ("many rows share", [(24, [9, 40, 130] * 8)], 2, 4, 1, True)])
+@pytest.mark.parametrize("scale", [0.0, 40.0])
+@pytest.mark.parametrize("at", [3, 60])
+def test_infinite_values_that_are_seen(gpu_lib, name, groups, kv, gq, q_len, cut, scale, at):
+    """A row that sees an infinite value gets it, whatever its weight (at a scale of 40 most vanish); NaN where it sees one, or
+    both infinities; the other dims are as they were."""
+    b = Batch(groups, 32, 96, kv, gq, q_len, seed=24)
+    page = int(b.tables[b.ids[0], at // 32])          # of the shared ones
+    cache = b.roomy() if cut else b.cache
+    inf = float("inf")
+    for shared in (True, False):
+        cache.pool.copy_(b.pool)
+        ref, zref = (t.clone() for t in b.run(shared, scale, cache=cache))
+        v = cache.pool[1, page, kv - 1]
+        v[at % 32, 7], v[at % 32, 95], v[at % 32, 40], v[at % 32 + 1, 64], v[at % 32 + 3, 64] = inf, -inf, float("nan"), inf, -inf
+        out, lse = b.run(shared, scale, cache=cache)
+        hit = out[:, (kv - 1) * gq:].float()
+        assert (hit[..., 7] == inf).all() and (hit[..., 95] == -inf).all()
+        assert torch.isnan(hit[..., 40]).all() and torch.isnan(hit[..., 64]).all()
+        keep = [i for i in range(96) if i not in (7, 95, 40, 64)]
+        assert torch.equal(out[..., keep], ref[..., keep]) and torch.equal(out[:, :(kv - 1) * gq], ref[:, :(kv - 1) * gq])
+        assert torch.equal(lse, zref)
