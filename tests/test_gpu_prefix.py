@@ -559,7 +559,7 @@ def test_one_short_request_in_a_run(gpu_lib):
     assert torch.equal(out, b.run(cache=cache)[0])
 
 
-@pytest.mark.parametrize("threads,samples,system,thread", [(8, 8, 32, 16), (3, 40, 40, 20), (40, 3, 16, 64), (2, 3, 16, 240)])
+@pytest.mark.parametrize("threads,samples,system,thread", [(8, 8, 32, 20), (3, 40, 40, 20), (40, 3, 16, 64), (2, 3, 16, 240)])
 def test_samples_of_threads(gpu_lib, threads, samples, system, thread):
     """Samples of several threads under one system prompt: what a thread's samples share is read once for each thread where
     that saves more than the system prompt read once for all."""
