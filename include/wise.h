@@ -597,6 +597,110 @@ wise_status wise_prefix_attn(const wise_cache* c, const wise_queries* a,
  * arguments). */
 size_t wise_prefix_workspace_bytes(const wise_cache* c, const wise_queries* a);
 
+/*
+ * The cache in 8 or 4 bits
+ * ------------------------
+ * The same cache, tables, lens and refs with pages that hold fewer bits than
+ * bf16: wise_cache_fork, _trim and _shared serve it as they are, and the calls
+ * below do what their namesakes do.  bits is 8 or 4.
+ *
+ * Dims 32 g .. 32 g + 31 of a token's head share a scale 2^e.  It is kept as
+ * the byte e + 127, and a value as a multiple of it: with 8 bits as E4M3 (sign, 4
+ * bits of exponent, 3 of mantissa, largest 448, no infinity, NaN where the
+ * other 7 bits are set), with 4 as E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6).  What the
+ * cache holds is exact in bf16.
+ *
+ *   pool   : [planes][pages][kv_heads][wise_qcache_page_bytes(c, bits)] bytes:
+ *            head_dim * bits / 8 bytes of codes for each of the page's tokens,
+ *            then head_dim / 32 scales for each.  Of two 4-bit codes in a byte the even
+ *            dim's is the low one.
+ *            keys   : a token's codes in the order of its dims, tokens one by one; the
+ *                     scales likewise.
+ *            values : the tokens in fours.  Of a four, the first sixteenth of the
+ *                     dims of its four tokens one by one, then the next sixteenth; of its
+ *                     scales, the first of the four tokens, then the next.
+ *
+ * A scale byte of 255 makes its 32 dims NaN.  Bytes 1 and 0, 253 and 254 are not
+ * written (nor, with 8 bits, any outside 10..246) and must not be held by tokens that are read.
+ */
+
+/* Bytes of one head's page, a multiple of 16 (0 for invalid arguments). */
+size_t wise_qcache_page_bytes(const wise_cache* c, int32_t bits);
+
+/*
+ * wise_qcache_append — wise_cache_append into such pages: quantises the newest
+ * counts[i] tokens of sequence seq_ids[i] in one layer.
+ *
+ * Of the 32 dims of a scale, with a their largest magnitude: e is the least whole
+ * number with a <= T 2^e, where T = 7 for 4 bits and 464 for 8 (so that a itself is off by at most
+ * half a step), within -125..125 for 4 bits and -117..119 for 8; a value
+ * x becomes the code nearest to x / 2^e, of two that are equally near the even one, the
+ * largest if x / 2^e is past it.  Where one of the 32 is infinite or NaN, all 32 are kept as NaN.
+ *
+ *   k_pool, v_pool : the layer's two planes; the others as for wise_cache_append.
+ * Errors: as wise_cache_append (WISE_ERR_UNSUPPORTED also for bits).
+ */
+wise_status wise_qcache_append(const wise_cache* c, int32_t bits, int32_t n,
+                               int32_t tokens, const int32_t* seq_ids,
+                               const int32_t* counts, const void* k,
+                               const void* v, const int32_t* tables,
+                               const int32_t* lens, void* k_pool, void* v_pool,
+                               void* hip_stream);
+
+/*
+ * wise_qcache_read — keys and values of one layer back in bf16: token t of entry i is
+ * position starts[i] + t of sequence seq_ids[i], t < counts[i].
+ *
+ *   counts : int32 [n], device; taken as min(max(counts[i], 0), tokens).
+ *   starts : int32 [n], device, or NULL: 0 for every entry.
+ *   k, v   : bf16 [n][kv_heads][tokens][head_dim], written; rows from counts[i] on, of
+ *            positions outside 0..lens-1, without a page, or of an id outside 0..seqs-1 are
+ *            left as they are.  An id may repeat.
+ * Errors: as wise_qcache_append.
+ */
+wise_status wise_qcache_read(const wise_cache* c, int32_t bits, int32_t n,
+                             int32_t tokens, const int32_t* seq_ids,
+                             const int32_t* counts, const int32_t* starts,
+                             const void* k_pool, const void* v_pool,
+                             const int32_t* tables, const int32_t* lens,
+                             void* k, void* v, void* hip_stream);
+
+/* wise_cache_reserve and wise_cache_compact for such a pool (the same
+ * workspace, wise_cache_workspace_bytes).  A copy of a last page copies whole fours of
+ * tokens. */
+wise_status wise_qcache_reserve(const wise_cache* c, int32_t bits, int32_t n,
+                                const int32_t* seq_ids, const int32_t* counts,
+                                int32_t* tables, int32_t* lens, int32_t* refs,
+                                int32_t* granted, void* pool, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
+wise_status wise_qcache_compact(const wise_cache* c, int32_t bits,
+                                int32_t* tables, int32_t* refs, void* pool,
+                                int32_t* live, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
+
+/*
+ * wise_qcache_attn — wise_prefix_attn over what such pages hold: the queries,
+ * the sums and the probabilities are as exact as there, only the keys and values are
+ * those that were kept.  A NaN value makes its dim NaN in every row that
+ * sees it, whatever its weight, and in no other; a NaN key the whole row.
+ *
+ *   workspace : wise_qcache_workspace_bytes(c, bits, a) bytes, 256-byte aligned.
+ * The others, and the errors, as for wise_prefix_attn (WISE_ERR_UNSUPPORTED
+ * also for bits).
+ */
+wise_status wise_qcache_attn(const wise_cache* c, int32_t bits,
+                             const wise_queries* a, const void* q,
+                             const void* k_pool, const void* v_pool,
+                             const int32_t* tables, const int32_t* lens,
+                             const int32_t* seq_ids, const int32_t* shared,
+                             void* o, float* lse, void* workspace,
+                             size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of device workspace wise_qcache_attn needs (0 for invalid
+ * arguments). */
+size_t wise_qcache_workspace_bytes(const wise_cache* c, int32_t bits,
+                                   const wise_queries* a);
+
 /* Static, NUL-terminated description of a status code. */
 const char* wise_status_string(wise_status st);
 

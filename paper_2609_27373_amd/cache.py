@@ -19,6 +19,10 @@ captured is kept for it.  No other call allocates when its output tensors
 are given.  Every call runs on the current stream of the cache's device, whichever
 device is current.  Graphs and streams that use one PagedCache share its buffers and
 must run in order.  A call on no sequences at all does nothing.
+
+QuantCache is the same cache held in 8 or 4 bits: append() quantises, attend()
+reads what was kept, read() gives it back in bf16, and everything else is as it was.
+Where PagedCache takes 4 head_dim bytes a token and key-value head, it takes 2 (head_dim bits / 8 + head_dim / 32).
 """
 
 from __future__ import annotations
@@ -42,13 +46,15 @@ class PagedCache:
         """`pool`, `tables`, `lens` and `refs` may be the caller's own buffers (of the layout in wise.h, in any
         valid state); those not given start out empty.  They stay the cache's for its life."""
         self.shape = wise.make_cache(pages, page, kv_heads, head_dim, 2 * layers, seqs, max_pages)
+        self._c = ctypes.byref(self.shape)
         n = wise.wise_cache_workspace_bytes(self.shape)
         if n == 0:
             raise ValueError(f"no such cache: layers {layers}, pages {pages}, page {page}, kv_heads {kv_heads}, "
                              f"head_dim {head_dim}, seqs {seqs}, max_pages {max_pages}")
         i32 = dict(dtype=_I32, device=device)
-        self._pool = self._own(pool, (2 * layers, pages, kv_heads, page, head_dim), _BF16, "pool",
-                               lambda s: torch.zeros(s, dtype=_BF16, device=device))
+        rows, dtype = self._page()
+        self._pool = self._own(pool, (2 * layers, pages, kv_heads, *rows), dtype, "pool",
+                               lambda s: torch.zeros(s, dtype=dtype, device=device))
         self._tables = self._own(tables, (seqs, max_pages), _I32, "tables", lambda s: torch.full(s, -1, **i32))
         self._lens = self._own(lens, (seqs,), _I32, "lens", lambda s: torch.zeros(s, **i32))
         self._refs = self._own(refs, (pages,), _I32, "refs", lambda s: torch.zeros(s, **i32))
@@ -61,7 +67,6 @@ class PagedCache:
         self._attend = {}                       # bytes that attend() needs, by (batch, heads, q_len)
         self._room, self._held = None, {}       # its workspace (address, bytes, tensor); those that graphs use, by address
         # The buffers above, checked once and for all, as the C calls take them.
-        self._c = ctypes.byref(self.shape)
         self._state = tuple(t.data_ptr() for t in (self._tables, self._lens, self._refs))
         self._ws = (self._workspace.data_ptr(), n)
 
@@ -69,6 +74,16 @@ class PagedCache:
     tables = property(lambda self: self._tables, doc="int32 [seqs][max_pages]")
     lens = property(lambda self: self._lens, doc="int32 [seqs]")
     refs = property(lambda self: self._refs, doc="int32 [pages]")
+
+    # What differs where the pages hold something else: the entry points, their first arguments, a page of one head.
+    _RESERVE, _APPEND, _COMPACT, _ATTEND = "wise_cache_reserve", "wise_cache_append", "wise_cache_compact", "wise_prefix_attn"
+    _kind = ()
+
+    def _page(self):
+        return (self.shape.page, self.shape.head_dim), _BF16
+
+    def _attend_bytes(self, queries):
+        return wise.wise_prefix_workspace_bytes(self.shape, queries)
 
     @staticmethod
     def _own(t, shape, dtype, name, make):
@@ -121,38 +136,42 @@ class PagedCache:
         """Room for counts[i] tokens more; returns the tokens granted (counts[i] or 0)."""
         n = seq_ids.numel()
         granted = self._ints(n) if granted is None else granted
-        self._call("wise_cache_reserve", n, self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n), *self._state,
+        self._call(self._RESERVE, *self._kind, n, self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n), *self._state,
                    self._arg(granted, _I32, "granted", n), self._pool.data_ptr(), *self._ws)
         return granted
 
     def append(self, layer, k, v, seq_ids, counts):
         """Writes the newest counts[i] tokens of each sequence in one layer; k, v: [n][kv_heads][tokens][head_dim]."""
-        c, n = self.shape, seq_ids.numel()
+        n = seq_ids.numel()
+        kp, vp, *args = self._rows(layer, k, v, seq_ids, counts, n)
+        if n > 0:
+            self._call(self._APPEND, *self._kind, n, k.shape[2], *args, *self._state[:2], kp, vp)
+
+    def _rows(self, layer, k, v, seq_ids, counts, n):
+        """Addresses of a layer's planes, and of the arguments that name rows of keys and values."""
+        c = self.shape
         if k.dim() != 4 or k.shape[0] != n or k.shape[1] != c.kv_heads or k.shape[3] != c.head_dim or v.shape != k.shape:
             raise ValueError(f"k and v must be [{n}][{c.kv_heads}][tokens][{c.head_dim}], got {tuple(k.shape)}, {tuple(v.shape)}")
-        kp, vp = self._layer(layer)
         rows = k.numel()
-        args = (self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n), self._arg(k, _BF16, "k", rows),
-                self._arg(v, _BF16, "v", rows))
-        if n > 0:
-            self._call("wise_cache_append", n, k.shape[2], *args, *self._state[:2], kp, vp)
+        return (*self._layer(layer), self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n),
+                self._arg(k, _BF16, "k", rows), self._arg(v, _BF16, "v", rows))
 
     def _layer(self, layer):
         if not 0 <= layer < self.shape.planes // 2:
             raise ValueError(f"layer {layer} of {self.shape.planes // 2}")
-        plane = self._pool.numel() // self.shape.planes * 2
+        plane = self._pool.numel() // self.shape.planes * self._pool.element_size()
         at = self._pool.data_ptr() + 2 * layer * plane
         return at, at + plane
 
     def layer(self, layer):
-        """The planes of one layer: (keys, values), [pages][kv_heads][page][head_dim]."""
+        """The planes of one layer: (keys, values), each as the pool without its first dimension."""
         self._layer(layer)
         return self._pool[2 * layer], self._pool[2 * layer + 1]
 
     def compact(self, live=None):
         """Moves the pages in use to the front of the pool; returns their number (int32 [1], on the device)."""
         live = self._ints(1) if live is None else live
-        self._call("wise_cache_compact", self._state[0], self._state[2], self._pool.data_ptr(), self._arg(live, _I32, "live", 1), *self._ws)
+        self._call(self._COMPACT, *self._kind, self._state[0], self._state[2], self._pool.data_ptr(), self._arg(live, _I32, "live", 1), *self._ws)
         return live
 
     def shared(self, seq_ids=None, min_pages=1, out=None):
@@ -175,7 +194,7 @@ class PagedCache:
         args = (self._arg(q, _BF16, "q", n), kp, vp, *self._state[:2], self._arg(seq_ids, _I32, "seq_ids", batch),
                 self._arg(shared, _I32, "shared", batch), self._arg(out, _BF16, "out", n), self._arg(lse, _F32, "lse", rows))
         if batch > 0:
-            self._call("wise_prefix_attn", ctypes.byref(wise.wise_queries(batch, heads, q_len, scale)), *args,
+            self._call(self._ATTEND, *self._kind, ctypes.byref(wise.wise_queries(batch, heads, q_len, scale)), *args,
                        *self._attend_workspace(batch, heads, q_len))
         return out
 
@@ -186,7 +205,7 @@ class PagedCache:
             # For a power of two of sequences, so that a growing batch grows it seldom (or for the batch itself, where
             # that many more are past a limit).
             sizes = ((1 << max(batch - 1, 0).bit_length(), heads, q_len), key)
-            n = next((x for x in (wise.wise_prefix_workspace_bytes(self.shape, wise.make_queries(*k)) for k in sizes) if x > 0), 0)
+            n = next((x for x in (self._attend_bytes(wise.make_queries(*k)) for k in sizes) if x > 0), 0)
             if n == 0:
                 return self._ws                 # for the call to refuse
             self._attend[key] = n
@@ -207,3 +226,36 @@ class PagedCache:
     def _capturing(self):
         with torch.cuda.device(self._index):
             return torch.cuda.is_current_stream_capturing()
+
+
+class QuantCache(PagedCache):
+    """A PagedCache whose keys and values are held in `bits` (8 or 4): 32 dims of a token's head share a power of two
+    as their scale, a value is an E4M3 or E2M1 multiple of it (wise.h says which, and where the bytes lie)."""
+
+    _RESERVE, _APPEND, _COMPACT, _ATTEND = "wise_qcache_reserve", "wise_qcache_append", "wise_qcache_compact", "wise_qcache_attn"
+
+    def __init__(self, layers, pages, page, kv_heads, head_dim, seqs, max_pages, bits=4, device="cuda", pool=None, tables=None,
+                 lens=None, refs=None):
+        """As PagedCache; a pool is uint8 [2 * layers][pages][kv_heads][bytes of a page]."""
+        if bits not in (4, 8):
+            raise ValueError(f"bits must be 4 or 8, got {bits!r}")
+        self.bits, self._kind = bits, (bits,)
+        super().__init__(layers, pages, page, kv_heads, head_dim, seqs, max_pages, device, pool, tables, lens, refs)
+
+    pool = property(lambda self: self._pool, doc="uint8 [2 * layers][pages][kv_heads][bytes of a page]")
+
+    def _page(self):
+        return (wise.wise_qcache_page_bytes(self.shape, self.bits),), torch.uint8
+
+    def _attend_bytes(self, queries):
+        return wise.wise_qcache_workspace_bytes(self.shape, self.bits, queries)
+
+    def read(self, layer, k, v, seq_ids, counts, starts=None):
+        """Positions starts[i] .. starts[i] + counts[i] - 1 (from 0 without starts) of each sequence in one layer, into
+        k, v: bf16 [n][kv_heads][tokens][head_dim]; other rows stay as they are."""
+        n = seq_ids.numel()
+        kp, vp, ids, counts, k_to, v_to = self._rows(layer, k, v, seq_ids, counts, n)
+        first = self._arg(starts, _I32, "starts", n)
+        if n > 0:
+            self._call("wise_qcache_read", self.bits, n, k.shape[2], ids, counts, first, kp, vp, *self._state[:2], k_to, v_to)
+        return k, v

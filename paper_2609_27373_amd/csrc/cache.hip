@@ -181,17 +181,25 @@ reserve_plan_kernel(Cache c, int n, const int32_t* __restrict__ ids, const int32
   }
 }
 
-// Copies rows * d bf16 of every plane and head of an entry's last page: kCopyHeads
-// of them a work-group, as many side by side as its threads reach, four passes in flight.
+// Copies what an entry's last page holds of its tokens, in every plane and head: their
+// rows, or (kept.hpp) the codes and scales of their fours.  kCopyHeads of them a work-group, as many side by side as its threads reach, four passes in flight.
 // The stores, here and below, pass the L2 by: nothing reads them before other kernels do.
 constexpr int kCopyHeads = 16;
 
+// 16-byte chunks of one head's page.
+__host__ __device__ __forceinline__ int page_chunks(const Cache& c, int bits) {
+  return c.page / 16 * (c.head_dim * bits / 8 + (bits == 16 ? 0 : c.head_dim / 32));
+}
+
+template <bool kBf16>
 __global__ void __launch_bounds__(256)
-reserve_copy_kernel(Cache c, const ReserveCopy* __restrict__ copies, uint16_t* pool) {
+reserve_copy_kernel(Cache c, int bits, const ReserveCopy* __restrict__ copies, uint16_t* pool) {
   const ReserveCopy r = copies[blockIdx.y];
   if (r.rows == 0) return;
-  const size_t head = (size_t)c.page * c.head_dim / 8, page = head * c.kv_heads;   // 16-byte chunks
-  const int chunks = r.rows * c.head_dim / 8, per = chunks < 256 ? 256 / chunks : 1;
+  const size_t head = kBf16 ? (size_t)c.page * c.head_dim / 8 : (size_t)page_chunks(c, bits), page = head * c.kv_heads;   // 16-byte chunks
+  const int fours = (r.rows + 3) / 4, codes = fours * c.head_dim * bits / 32;      // codes of the fours, 16 bytes each
+  const int apart = c.page * c.head_dim * bits / 128 - codes;                      // chunks between these and their scales
+  const int chunks = kBf16 ? r.rows * c.head_dim / 8 : codes + (fours * c.head_dim / 8 + 15) / 16, per = chunks < 256 ? 256 / chunks : 1;
   const int mine = chunks < 256 ? threadIdx.x / chunks : 0;
   if (mine >= per) return;
   const uint32_t x0 = blockIdx.x * kCopyHeads, all = (uint32_t)(c.planes * c.kv_heads), x1 = min(x0 + kCopyHeads, all);
@@ -203,7 +211,7 @@ reserve_copy_kernel(Cache c, const ReserveCopy* __restrict__ copies, uint16_t* p
       for (int u = 0; u < 4; ++u) {
         const uint32_t y = x + u * per, plane = y / (uint32_t)c.kv_heads, h = y - plane * c.kv_heads;
         if (y < x1) {
-          u32x4_t* base = (u32x4_t*)pool + (size_t)plane * c.pages * page + h * head + ch;
+          u32x4_t* base = (u32x4_t*)pool + (size_t)plane * c.pages * page + h * head + (kBf16 || ch < codes ? ch : ch + apart);
           to[u] = base + (size_t)r.dst * page;
           w[u] = base[(size_t)r.src * page];
         }
@@ -314,7 +322,7 @@ compact_plan_kernel(Cache c, int32_t* refs, int32_t* live, int32_t* plan, int32_
 
 __global__ void __launch_bounds__(256)
 compact_move_kernel(Cache c, const int32_t* __restrict__ plan, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                    const int32_t* __restrict__ renamed, int32_t* tables, u32x4_t* pool) {
+                    const int32_t* __restrict__ renamed, int32_t* tables, u32x4_t* pool, int64_t page) {
   const int used = plan[0], moves = plan[1];
   if (moves == 0) return;
   const size_t entries = (size_t)c.seqs * c.max_pages;
@@ -322,7 +330,7 @@ compact_move_kernel(Cache c, const int32_t* __restrict__ plan, const int32_t* __
     const int p = tables[e];
     if (p >= used && p < c.pages) tables[e] = renamed[p];
   }
-  const int64_t page = (int64_t)c.kv_heads * c.page * c.head_dim / 8;   // 16-byte chunks of a page in one plane
+  // page: 16-byte chunks of a page in one plane
   const int64_t pieces = (page + 1023) / 1024, items = moves * (int64_t)c.planes * pieces;
   for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
     const int64_t piece = x % pieces, y = x / pieces, plane = y % c.planes, m = y / c.planes;
@@ -393,14 +401,15 @@ hipError_t launch_cache_trim(const Cache& c, int n, const int32_t* ids, const in
   return hipGetLastError();
 }
 
-hipError_t launch_cache_reserve(const Cache& c, int n, const int32_t* ids, const int32_t* counts, int32_t* tables, int32_t* lens,
+hipError_t launch_cache_reserve(const Cache& c, int bits, int n, const int32_t* ids, const int32_t* counts, int32_t* tables, int32_t* lens,
                                 int32_t* refs, int32_t* granted, void* pool, void* ws, hipStream_t st) {
   const CacheSpace w = cache_space(c, ws);
   reserve_plan_kernel<<<1, kPlan, 0, st>>>(c, n, ids, counts, tables, lens, refs, granted, w.src, w.copies);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)((c.planes * c.kv_heads + kCopyHeads - 1) / kCopyHeads), n);
-  reserve_copy_kernel<<<grid, 256, 0, st>>>(c, w.copies, (uint16_t*)pool);
+  if (bits == 16) reserve_copy_kernel<true><<<grid, 256, 0, st>>>(c, bits, w.copies, (uint16_t*)pool);
+  else reserve_copy_kernel<false><<<grid, 256, 0, st>>>(c, bits, w.copies, (uint16_t*)pool);
   return hipGetLastError();
 }
 
@@ -421,13 +430,13 @@ hipError_t launch_cache_append(const Cache& c, int n, int tokens, const int32_t*
   return c.head_dim == 64 ? run(append_tile_kernel<64>) : c.head_dim == 96 ? run(append_tile_kernel<96>) : run(append_tile_kernel<128>);
 }
 
-hipError_t launch_cache_compact(const Cache& c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,
+hipError_t launch_cache_compact(const Cache& c, int bits, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,
                                 hipStream_t st) {
   const CacheSpace w = cache_space(c, ws);
   compact_plan_kernel<<<1, kPlan, 0, st>>>(c, refs, live, w.plan, w.src, w.dst, w.renamed);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  compact_move_kernel<<<2048, 256, 0, st>>>(c, w.plan, w.src, w.dst, w.renamed, tables, (u32x4_t*)pool);
+  compact_move_kernel<<<2048, 256, 0, st>>>(c, w.plan, w.src, w.dst, w.renamed, tables, (u32x4_t*)pool, (int64_t)c.kv_heads * page_chunks(c, bits));
   return hipGetLastError();
 }
 

@@ -1,0 +1,91 @@
+// kept.hpp — keys and values held in 8 or 4 bits: where the bytes of a page lie, and
+// how they become bf16.
+//
+// 32 dims of a token's head share a scale 2^e, kept as the byte e + 127 (255: all 32
+// are NaN); a value is a multiple of it with 8 bits (E4M3) or 4 (E2M1, the even dim
+// in the low half of a byte).  A page of one head is the codes of its tokens, then their
+// scales.  Keys lie token by token.  Values lie in fours of tokens, of which
+// each sixteenth of a head's dims, or each scale, comes in turn: what a lane of the
+// attention multiplies, four tokens at D / 16 dims, is then consecutive bytes, and
+// what a wave loads of 16 tokens, keys or values, is one stretch in lane order.
+#pragma once
+
+#include "wise_device.hpp"
+
+namespace wise {
+
+template <int D, int B>
+struct Kept {
+  static constexpr int kRow = D * B / 8;              // bytes of a token's codes
+  static constexpr int kScales = D / 32;              // and scales
+  static constexpr int kPiece = kRow / 4;             // bytes of a lane: a quarter of a key, or four tokens' sixteenths
+  static constexpr int kWords = kPiece / 4;
+  static constexpr int kPairs = D / 32;               // pairs of dims of a token's sixteenth
+
+  // Byte of dim d of token t's codes, and of its scale of dims 32 g ..., behind the page's codes.
+  __device__ static int v_code(int t, int d) {
+    const int j = d * B / 8, piece = kRow / 16;
+    return (t >> 2) * 4 * kRow + j / piece * kPiece + (t & 3) * piece + j % piece;
+  }
+  __device__ static int v_scale(int t, int g) { return ((t >> 2) * kScales + g) * 4 + (t & 3); }
+};
+
+inline int kept_key_bytes(int d, int bits) { return 2 * (d * bits / 8 + d / 32); }   // of K and V, a key and key-value head
+
+// Two values of a word as bf16: number i of its bytes (B = 4) or half words (B = 8).  Only
+// the exponent of `scale` counts, whatever its other bits; 255 makes NaN of any code.
+template <int B>
+__device__ __forceinline__ uint32_t widen_pair(uint32_t w, float scale, int i) {
+  bf16x2_t r;
+  if constexpr (B == 4) {
+    r = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+        : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  } else {
+    r = i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+// Pair i of consecutive words.
+template <int B>
+__device__ __forceinline__ uint32_t widen_at(const uint32_t* w, float scale, int i) {
+  constexpr int kPer = B == 4 ? 4 : 2;
+  return widen_pair<B>(w[i / kPer], scale, i % kPer);
+}
+
+// Scale byte i of a word, as widen_pair takes it.
+__device__ __forceinline__ float scale_of(uint32_t w, int i) {
+  return __builtin_bit_cast(float, i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1);
+}
+
+// The bytes of w that are 255, and (kCode) those whose lower seven bits are set, as 255.
+template <bool kCode>
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & (kCode ? 0x80808080u : 0x80808080u & w);
+  return (t >> 7) * 255u;
+}
+
+// N words at p, which is aligned as a lane's bytes are.
+template <int N>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  typedef uint32_t W2 __attribute__((ext_vector_type(2), aligned(8)));
+  typedef uint32_t W3 __attribute__((ext_vector_type(3), aligned(4)));
+  typedef uint32_t W4 __attribute__((ext_vector_type(4), aligned(8)));
+  static_assert(N == 2 || N == 3 || N == 4 || N == 6 || N == 8, "words of a lane");
+  if constexpr (N >= 4) {
+    const W4 x = *(const W4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = x[i];
+    if constexpr (N > 4) load_words<N - 4>(p + 16, w + 4);
+  } else if constexpr (N == 3) {
+    const W3 x = *(const W3*)p;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w[i] = x[i];
+  } else {
+    const W2 x = *(const W2*)p;
+    w[0] = x[0], w[1] = x[1];
+  }
+}
+
+}  // namespace wise

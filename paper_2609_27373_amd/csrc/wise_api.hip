@@ -104,6 +104,75 @@ wise_status check_ints(std::initializer_list<const void*> ps) {
 
 wise_status from_hip(hipError_t e) { return e == hipSuccess ? WISE_OK : WISE_ERR_HIP; }
 
+// What a call that moves tokens' keys and values into or out of one layer is given.
+wise_status check_rows(const wise_cache* c, int32_t n, int32_t tokens, const int32_t* seq_ids, const int32_t* counts, const void* k,
+                       const void* v, const int32_t* tables, const int32_t* lens, const void* k_pool, const void* v_pool,
+                       wise::Cache* d) {
+  wise_status st = check_entries(c, n, d);
+  if (st != WISE_OK) return st;
+  if (tokens < 1) return WISE_ERR_SHAPE;
+  if (n == 0) return WISE_OK;
+  if ((st = check_ints({seq_ids, counts, tables, lens})) != WISE_OK) return st;
+  if ((st = check_qkvo(k, v, k_pool, v_pool)) != WISE_OK) return st;
+  return (int64_t)n * d->kv_heads > kMaxAppendRows / tokens ? WISE_ERR_SHAPE : WISE_OK;
+}
+
+// A cache held in 8 or 4 bits.
+wise_status check_kept(const wise_cache* c, int32_t bits) {
+  wise::Cache d;
+  const wise_status st = check_cache(c, &d);
+  return st != WISE_OK ? st : bits == 4 || bits == 8 ? WISE_OK : WISE_ERR_UNSUPPORTED;
+}
+
+// The calls that differ only in what the pages hold (bits: 16 for bf16).
+wise_status reserve(const wise_cache* c, int32_t bits, int32_t n, const int32_t* seq_ids, const int32_t* counts, int32_t* tables,
+                               int32_t* lens, int32_t* refs, int32_t* granted, void* pool, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_entries(c, n, &d);
+  if (st != WISE_OK || n == 0) return st;
+  if (!pool || !workspace) return WISE_ERR_NULL;
+  if ((st = check_ints({seq_ids, counts, tables, lens, refs, granted})) != WISE_OK) return st;
+  if (!aligned(pool, 16) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
+  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
+  return from_hip(wise::launch_cache_reserve(d, bits, n, seq_ids, counts, tables, lens, refs, granted, pool, workspace,
+                                             (hipStream_t)hip_stream));
+}
+
+wise_status compact(const wise_cache* c, int32_t bits, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_cache(c, &d);
+  if (st != WISE_OK) return st;
+  if (!pool || !workspace) return WISE_ERR_NULL;
+  if ((st = check_ints({tables, refs})) != WISE_OK) return st;
+  if (!aligned(pool, 16) || (live && !aligned(live, 4)) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
+  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
+  return from_hip(wise::launch_cache_compact(d, bits, tables, refs, pool, live, workspace, (hipStream_t)hip_stream));
+}
+
+wise_status attend(const wise_cache* c, int32_t bits, const wise_queries* a, const void* q, const void* k_pool, const void* v_pool,
+                             const int32_t* tables, const int32_t* lens, const int32_t* seq_ids, const int32_t* shared, void* o,
+                             float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  wise::Cache d;
+  wise::Queries x;
+  wise_status st = check_queries(c, a, &d, &x);
+  if (st != WISE_OK) return st;
+  if (seq_ids == nullptr && x.batch > d.seqs) return WISE_ERR_SHAPE;
+  if ((st = check_qkvo(q, k_pool, v_pool, o)) != WISE_OK) return st;
+  if ((st = check_ints({tables, lens})) != WISE_OK) return st;
+  if (!workspace) return WISE_ERR_NULL;
+  if ((seq_ids && !aligned(seq_ids, 4)) || (shared && !aligned(shared, 4)) || (lse && !aligned(lse, 4)) ||
+      !aligned(workspace, 256))
+    return WISE_ERR_SHAPE;
+  if (workspace_bytes < (bits == 16 ? wise::prefix_workspace_bytes(d, x) : wise::qprefix_workspace_bytes(d, x))) return WISE_ERR_WORKSPACE;
+  if (bits != 16)
+    return from_hip(wise::launch_qprefix(d, bits, x, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace,
+                                         (hipStream_t)hip_stream));
+  return from_hip(wise::launch_prefix(d, x, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace,
+                                      (hipStream_t)hip_stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -336,42 +405,22 @@ wise_status wise_cache_trim(const wise_cache* c, int32_t n, const int32_t* seq_i
 wise_status wise_cache_reserve(const wise_cache* c, int32_t n, const int32_t* seq_ids, const int32_t* counts, int32_t* tables,
                                int32_t* lens, int32_t* refs, int32_t* granted, void* pool, void* workspace,
                                size_t workspace_bytes, void* hip_stream) {
-  wise::Cache d;
-  wise_status st = check_entries(c, n, &d);
-  if (st != WISE_OK || n == 0) return st;
-  if (!pool || !workspace) return WISE_ERR_NULL;
-  if ((st = check_ints({seq_ids, counts, tables, lens, refs, granted})) != WISE_OK) return st;
-  if (!aligned(pool, 16) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
-  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
-  return from_hip(wise::launch_cache_reserve(d, n, seq_ids, counts, tables, lens, refs, granted, pool, workspace,
-                                             (hipStream_t)hip_stream));
+  return reserve(c, 16, n, seq_ids, counts, tables, lens, refs, granted, pool, workspace, workspace_bytes, hip_stream);
 }
 
 wise_status wise_cache_append(const wise_cache* c, int32_t n, int32_t tokens, const int32_t* seq_ids, const int32_t* counts,
                               const void* k, const void* v, const int32_t* tables, const int32_t* lens, void* k_pool,
                               void* v_pool, void* hip_stream) {
   wise::Cache d;
-  wise_status st = check_entries(c, n, &d);
-  if (st != WISE_OK) return st;
-  if (tokens < 1) return WISE_ERR_SHAPE;
-  if (n == 0) return WISE_OK;
-  if ((st = check_ints({seq_ids, counts, tables, lens})) != WISE_OK) return st;
-  if ((st = check_qkvo(k, v, k_pool, v_pool)) != WISE_OK) return st;
-  if ((int64_t)n * d.kv_heads > kMaxAppendRows / tokens) return WISE_ERR_SHAPE;
+  const wise_status st = check_rows(c, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool, &d);
+  if (st != WISE_OK || n == 0) return st;
   return from_hip(wise::launch_cache_append(d, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
                                             (hipStream_t)hip_stream));
 }
 
 wise_status wise_cache_compact(const wise_cache* c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* workspace,
                                size_t workspace_bytes, void* hip_stream) {
-  wise::Cache d;
-  wise_status st = check_cache(c, &d);
-  if (st != WISE_OK) return st;
-  if (!pool || !workspace) return WISE_ERR_NULL;
-  if ((st = check_ints({tables, refs})) != WISE_OK) return st;
-  if (!aligned(pool, 16) || (live && !aligned(live, 4)) || !aligned(workspace, 256)) return WISE_ERR_SHAPE;
-  if (workspace_bytes < wise::cache_workspace_bytes(d)) return WISE_ERR_WORKSPACE;
-  return from_hip(wise::launch_cache_compact(d, tables, refs, pool, live, workspace, (hipStream_t)hip_stream));
+  return compact(c, 16, tables, refs, pool, live, workspace, workspace_bytes, hip_stream);
 }
 
 wise_status wise_cache_shared(const wise_cache* c, int32_t batch, int32_t min_pages, const int32_t* seq_ids,
@@ -393,26 +442,68 @@ size_t wise_cache_workspace_bytes(const wise_cache* c) {
 wise_status wise_prefix_attn(const wise_cache* c, const wise_queries* a, const void* q, const void* k_pool, const void* v_pool,
                              const int32_t* tables, const int32_t* lens, const int32_t* seq_ids, const int32_t* shared, void* o,
                              float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  wise::Cache d;
-  wise::Queries x;
-  wise_status st = check_queries(c, a, &d, &x);
-  if (st != WISE_OK) return st;
-  if (seq_ids == nullptr && x.batch > d.seqs) return WISE_ERR_SHAPE;
-  if ((st = check_qkvo(q, k_pool, v_pool, o)) != WISE_OK) return st;
-  if ((st = check_ints({tables, lens})) != WISE_OK) return st;
-  if (!workspace) return WISE_ERR_NULL;
-  if ((seq_ids && !aligned(seq_ids, 4)) || (shared && !aligned(shared, 4)) || (lse && !aligned(lse, 4)) ||
-      !aligned(workspace, 256))
-    return WISE_ERR_SHAPE;
-  if (workspace_bytes < wise::prefix_workspace_bytes(d, x)) return WISE_ERR_WORKSPACE;
-  return from_hip(wise::launch_prefix(d, x, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace,
-                                      (hipStream_t)hip_stream));
+  return attend(c, 16, a, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace, workspace_bytes, hip_stream);
 }
 
 size_t wise_prefix_workspace_bytes(const wise_cache* c, const wise_queries* a) {
   wise::Cache d;
   wise::Queries x;
   return check_queries(c, a, &d, &x) == WISE_OK ? wise::prefix_workspace_bytes(d, x) : 0;
+}
+
+wise_status wise_qcache_reserve(const wise_cache* c, int32_t bits, int32_t n, const int32_t* seq_ids, const int32_t* counts,
+                                int32_t* tables, int32_t* lens, int32_t* refs, int32_t* granted, void* pool, void* workspace,
+                                size_t workspace_bytes, void* hip_stream) {
+  const wise_status st = check_kept(c, bits);
+  return st != WISE_OK ? st
+                       : reserve(c, bits, n, seq_ids, counts, tables, lens, refs, granted, pool, workspace, workspace_bytes, hip_stream);
+}
+
+wise_status wise_qcache_compact(const wise_cache* c, int32_t bits, int32_t* tables, int32_t* refs, void* pool, int32_t* live,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const wise_status st = check_kept(c, bits);
+  return st != WISE_OK ? st : compact(c, bits, tables, refs, pool, live, workspace, workspace_bytes, hip_stream);
+}
+
+wise_status wise_qcache_append(const wise_cache* c, int32_t bits, int32_t n, int32_t tokens, const int32_t* seq_ids,
+                               const int32_t* counts, const void* k, const void* v, const int32_t* tables, const int32_t* lens,
+                               void* k_pool, void* v_pool, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_kept(c, bits);
+  if (st != WISE_OK) return st;
+  if ((st = check_rows(c, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool, &d)) != WISE_OK || n == 0) return st;
+  return from_hip(wise::launch_qcache_append(d, bits, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
+                                             (hipStream_t)hip_stream));
+}
+
+wise_status wise_qcache_read(const wise_cache* c, int32_t bits, int32_t n, int32_t tokens, const int32_t* seq_ids,
+                             const int32_t* counts, const int32_t* starts, const void* k_pool, const void* v_pool,
+                             const int32_t* tables, const int32_t* lens, void* k, void* v, void* hip_stream) {
+  wise::Cache d;
+  wise_status st = check_kept(c, bits);
+  if (st != WISE_OK) return st;
+  if ((st = check_rows(c, n, tokens, seq_ids, counts, k, v, tables, lens, k_pool, v_pool, &d)) != WISE_OK || n == 0) return st;
+  if (starts && !aligned(starts, 4)) return WISE_ERR_SHAPE;
+  return from_hip(wise::launch_qcache_read(d, bits, n, tokens, seq_ids, counts, starts, k_pool, v_pool, tables, lens, k, v,
+                                           (hipStream_t)hip_stream));
+}
+
+wise_status wise_qcache_attn(const wise_cache* c, int32_t bits, const wise_queries* a, const void* q, const void* k_pool,
+                             const void* v_pool, const int32_t* tables, const int32_t* lens, const int32_t* seq_ids,
+                             const int32_t* shared, void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const wise_status st = check_kept(c, bits);
+  return st != WISE_OK ? st
+                       : attend(c, bits, a, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse, workspace, workspace_bytes, hip_stream);
+}
+
+size_t wise_qcache_workspace_bytes(const wise_cache* c, int32_t bits, const wise_queries* a) {
+  wise::Cache d;
+  wise::Queries x;
+  return check_kept(c, bits) == WISE_OK && check_queries(c, a, &d, &x) == WISE_OK ? wise::qprefix_workspace_bytes(d, x) : 0;
+}
+
+size_t wise_qcache_page_bytes(const wise_cache* c, int32_t bits) {
+  return check_kept(c, bits) == WISE_OK ? (size_t)c->page * (c->head_dim * bits / 8 + c->head_dim / 32) : 0;
 }
 
 const char* wise_status_string(wise_status st) {

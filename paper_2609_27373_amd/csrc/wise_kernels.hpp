@@ -70,11 +70,12 @@ hipError_t launch_cache_fork(const Cache& c, int n, const int32_t* src, const in
                              int32_t* refs, int32_t* done, hipStream_t st);
 hipError_t launch_cache_trim(const Cache& c, int n, const int32_t* ids, const int32_t* new_lens, int32_t* tables, int32_t* lens,
                              int32_t* refs, hipStream_t st);
-hipError_t launch_cache_reserve(const Cache& c, int n, const int32_t* ids, const int32_t* counts, int32_t* tables, int32_t* lens,
+// bits: 16 for a pool in bf16, 8 or 4 for one of kept.hpp.
+hipError_t launch_cache_reserve(const Cache& c, int bits, int n, const int32_t* ids, const int32_t* counts, int32_t* tables, int32_t* lens,
                                 int32_t* refs, int32_t* granted, void* pool, void* ws, hipStream_t st);
 hipError_t launch_cache_append(const Cache& c, int n, int tokens, const int32_t* ids, const int32_t* counts, const void* k,
                                const void* v, const int32_t* tables, const int32_t* lens, void* kp, void* vp, hipStream_t st);
-hipError_t launch_cache_compact(const Cache& c, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,
+hipError_t launch_cache_compact(const Cache& c, int bits, int32_t* tables, int32_t* refs, void* pool, int32_t* live, void* ws,
                                 hipStream_t st);
 hipError_t launch_cache_shared(const Cache& c, int batch, int min_pages, const int32_t* ids, const int32_t* tables,
                                const int32_t* lens, int32_t* shared, hipStream_t st);
@@ -83,5 +84,13 @@ hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const 
                          const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse, void* ws,
                          hipStream_t st);
 size_t prefix_workspace_bytes(const Cache& c, const Queries& a);
+
+hipError_t launch_qcache_append(const Cache& c, int bits, int n, int tokens, const int32_t* ids, const int32_t* counts, const void* k,
+                                const void* v, const int32_t* tables, const int32_t* lens, void* kp, void* vp, hipStream_t st);
+hipError_t launch_qcache_read(const Cache& c, int bits, int n, int tokens, const int32_t* ids, const int32_t* counts, const int32_t* starts,
+                              const void* kp, const void* vp, const int32_t* tables, const int32_t* lens, void* k, void* v, hipStream_t st);
+hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void* q, const void* kp, const void* vp, const int32_t* tables,
+                          const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse, void* ws, hipStream_t st);
+size_t qprefix_workspace_bytes(const Cache& c, const Queries& a);
 
 }  // namespace wise

@@ -36,6 +36,8 @@ EXPORTS = ("wise_dense_attn_accum", "wise_select_support", "wise_select_support_
            "wise_support_capacity", "wise_cache_fork", "wise_cache_trim", "wise_cache_reserve",
            "wise_cache_append", "wise_cache_compact", "wise_cache_shared",
            "wise_cache_workspace_bytes", "wise_prefix_attn", "wise_prefix_workspace_bytes",
+           "wise_qcache_page_bytes", "wise_qcache_append", "wise_qcache_read", "wise_qcache_reserve",
+           "wise_qcache_compact", "wise_qcache_attn", "wise_qcache_workspace_bytes",
            "wise_status_string", "wise_abi_version")
 
 
@@ -138,13 +140,22 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                      ("wise_cache_append", [C, I, I, P, P, P, P, P, P, P, P, P]),
                      ("wise_cache_compact", [C, P, P, P, P, P, Z, P]),
                      ("wise_cache_shared", [C, I, I, P, P, P, P, P]),
-                     ("wise_prefix_attn", [C, Q, P, P, P, P, P, P, P, P, P, P, Z, P])):
+                     ("wise_prefix_attn", [C, Q, P, P, P, P, P, P, P, P, P, P, Z, P]),
+                     ("wise_qcache_append", [C, I, I, I, P, P, P, P, P, P, P, P, P]),
+                     ("wise_qcache_read", [C, I, I, I, P, P, P, P, P, P, P, P, P, P]),
+                     ("wise_qcache_reserve", [C, I, I, P, P, P, P, P, P, P, P, Z, P]),
+                     ("wise_qcache_compact", [C, I, P, P, P, P, P, Z, P]),
+                     ("wise_qcache_attn", [C, I, Q, P, P, P, P, P, P, P, P, P, P, Z, P])):
         getattr(lib, fn).argtypes = args
         getattr(lib, fn).restype = ctypes.c_int
     lib.wise_cache_workspace_bytes.argtypes = [C]
     lib.wise_cache_workspace_bytes.restype = Z
     lib.wise_prefix_workspace_bytes.argtypes = [C, Q]
     lib.wise_prefix_workspace_bytes.restype = Z
+    lib.wise_qcache_page_bytes.argtypes = [C, I]
+    lib.wise_qcache_page_bytes.restype = Z
+    lib.wise_qcache_workspace_bytes.argtypes = [C, I, Q]
+    lib.wise_qcache_workspace_bytes.restype = Z
     lib.wise_status_string.argtypes = [ctypes.c_int]
     lib.wise_status_string.restype = ctypes.c_char_p
     lib.wise_abi_version.argtypes = []
@@ -445,6 +456,85 @@ def wise_cache_workspace_bytes(c: wise_cache) -> int:
 
 def wise_prefix_workspace_bytes(c: wise_cache, a: wise_queries) -> int:
     return int(_lib().wise_prefix_workspace_bytes(ctypes.byref(c), ctypes.byref(a)))
+
+
+def _kept_numel(c: wise_cache, bits: int) -> int:
+    """Bytes of one plane of a pool in 8 or 4 bits (0 for invalid arguments, which the library then rejects)."""
+    return c.pages * c.kv_heads * wise_qcache_page_bytes(c, bits)
+
+
+def wise_qcache_page_bytes(c: wise_cache, bits: int) -> int:
+    return int(_lib().wise_qcache_page_bytes(ctypes.byref(c), bits))
+
+
+def wise_qcache_append(c: wise_cache, bits: int, tokens: int, seq_ids, counts, k, v, tables, lens, k_pool, v_pool,
+                       stream=None) -> None:
+    _, nt, ns, _ = _cache_numel(c)
+    i32, bf, u8 = torch.int32, torch.bfloat16, torch.uint8
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    rows, plane = n * c.kv_heads * tokens * c.head_dim, _kept_numel(c, bits)
+    _check(_lib().wise_qcache_append(
+        ctypes.byref(c), bits, n, tokens, ps, _ptr(counts, i32, "counts", n), _ptr(k, bf, "k", rows),
+        _ptr(v, bf, "v", rows), _ptr(tables, i32, "tables", nt), _ptr(lens, i32, "lens", ns),
+        _ptr(k_pool, u8, "k_pool", plane), _ptr(v_pool, u8, "v_pool", plane), _stream(stream)),
+        "wise_qcache_append")
+
+
+def wise_qcache_read(c: wise_cache, bits: int, tokens: int, seq_ids, counts, starts, k_pool, v_pool, tables, lens, k, v,
+                     stream=None) -> None:
+    _, nt, ns, _ = _cache_numel(c)
+    i32, bf, u8 = torch.int32, torch.bfloat16, torch.uint8
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    rows, plane = n * c.kv_heads * tokens * c.head_dim, _kept_numel(c, bits)
+    _check(_lib().wise_qcache_read(
+        ctypes.byref(c), bits, n, tokens, ps, _ptr(counts, i32, "counts", n), _ptr(starts, i32, "starts", n),
+        _ptr(k_pool, u8, "k_pool", plane), _ptr(v_pool, u8, "v_pool", plane), _ptr(tables, i32, "tables", nt),
+        _ptr(lens, i32, "lens", ns), _ptr(k, bf, "k", rows), _ptr(v, bf, "v", rows), _stream(stream)),
+        "wise_qcache_read")
+
+
+def wise_qcache_reserve(c: wise_cache, bits: int, seq_ids, counts, tables, lens, refs, granted, pool, workspace,
+                        stream=None) -> None:
+    _, nt, ns, nr = _cache_numel(c)
+    i32 = torch.int32
+    n, ps = _entries(seq_ids, None, "seq_ids")
+    ws_bytes = workspace.numel() * workspace.element_size()
+    _check(_lib().wise_qcache_reserve(
+        ctypes.byref(c), bits, n, ps, _ptr(counts, i32, "counts", n), _ptr(tables, i32, "tables", nt),
+        _ptr(lens, i32, "lens", ns), _ptr(refs, i32, "refs", nr), _ptr(granted, i32, "granted", n),
+        _ptr(pool, torch.uint8, "pool", _kept_numel(c, bits) * c.planes), _ptr(workspace, None, "workspace"),
+        ctypes.c_size_t(ws_bytes), _stream(stream)), "wise_qcache_reserve")
+
+
+def wise_qcache_compact(c: wise_cache, bits: int, tables, refs, pool, live=None, workspace=None, stream=None) -> None:
+    _, nt, _, nr = _cache_numel(c)
+    i32 = torch.int32
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().wise_qcache_compact(
+        ctypes.byref(c), bits, _ptr(tables, i32, "tables", nt), _ptr(refs, i32, "refs", nr),
+        _ptr(pool, torch.uint8, "pool", _kept_numel(c, bits) * c.planes), _ptr(live, i32, "live", 1),
+        _ptr(workspace, None, "workspace"), ctypes.c_size_t(ws_bytes), _stream(stream)),
+        "wise_qcache_compact")
+
+
+def wise_qcache_attn(c: wise_cache, bits: int, a: wise_queries, q, k_pool, v_pool, tables, lens, seq_ids, shared, o, lse=None,
+                     workspace=None, stream=None) -> None:
+    _, nt, ns, _ = _cache_numel(c)
+    i32, bf, u8 = torch.int32, torch.bfloat16, torch.uint8
+    rows, plane = a.batch * a.heads * a.q_len, _kept_numel(c, bits)
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().wise_qcache_attn(
+        ctypes.byref(c), bits, ctypes.byref(a), _ptr(q, bf, "q", rows * c.head_dim),
+        _ptr(k_pool, u8, "k_pool", plane), _ptr(v_pool, u8, "v_pool", plane),
+        _ptr(tables, i32, "tables", nt), _ptr(lens, i32, "lens", ns),
+        _ptr(seq_ids, i32, "seq_ids", a.batch), _ptr(shared, i32, "shared", a.batch),
+        _ptr(o, bf, "o", rows * c.head_dim), _ptr(lse, torch.float32, "lse", rows),
+        _ptr(workspace, None, "workspace"), ctypes.c_size_t(ws_bytes), _stream(stream)),
+        "wise_qcache_attn")
+
+
+def wise_qcache_workspace_bytes(c: wise_cache, bits: int, a: wise_queries) -> int:
+    return int(_lib().wise_qcache_workspace_bytes(ctypes.byref(c), bits, ctypes.byref(a)))
 
 
 def wise_status_string(status: int) -> str:
