@@ -32,26 +32,40 @@ struct Kept {
 
 inline int kept_key_bytes(int d, int bits) { return 2 * (d * bits / 8 + d / 32); }   // of K and V, a key and key-value head
 
-// Two values of a word as bf16: number i of its bytes (B = 4) or half words (B = 8).  Only
+// Two values of a word as bf16 (or kHalf: as fp16): number i of its bytes (B = 4) or half words (B = 8).  Only
 // the exponent of `scale` counts, whatever its other bits; 255 makes NaN of any code.
-template <int B>
+template <int B, bool kHalf = false>
 __device__ __forceinline__ uint32_t widen_pair(uint32_t w, float scale, int i) {
-  bf16x2_t r;
-  if constexpr (B == 4) {
-    r = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
-        : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
-        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
-                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  if constexpr (B == 4 && !kHalf) {
+    return __builtin_bit_cast(uint32_t, i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+                                        : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+                                        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  } else if constexpr (B == 4) {
+    return __builtin_bit_cast(uint32_t, i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)
+                                        : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)
+                                        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3));
+  } else if constexpr (!kHalf) {
+    return __builtin_bit_cast(uint32_t, i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
   } else {
-    r = i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
+    return __builtin_bit_cast(uint32_t, i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true));
   }
-  return __builtin_bit_cast(uint32_t, r);
 }
 // Pair i of consecutive words.
-template <int B>
+template <int B, bool kHalf = false>
 __device__ __forceinline__ uint32_t widen_at(const uint32_t* w, float scale, int i) {
   constexpr int kPer = B == 4 ? 4 : 2;
-  return widen_pair<B>(w[i / kPer], scale, i % kPer);
+  return widen_pair<B, kHalf>(w[i / kPer], scale, i % kPer);
+}
+
+// Nonzero bits where one of a word's scales makes products that fp16 does not hold exactly: it does
+// with e from -23 to 8 for 4 bits (0.5 to 6 times 2^e), from -15 to 0 (of what would do to 7) for 8 (2^-9 to 448).
+template <int B>
+__device__ __forceinline__ uint32_t past_half(uint32_t w) {
+  return B == 4 ? ((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u : (w ^ 0x70707070u) & 0xf0f0f0f0u;
 }
 
 // Scale byte i of a word, as widen_pair takes it.

@@ -403,7 +403,7 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
       else if (more) copy_k(fk, it + 2, i - kC);
     };
     if (active) {
-      w.template step<2, true, true, 0, true>(sk + (b ^ 1) * kT, sv + b * kT, ra, lane, x.sc, sc, sn, mx,
+      w.template step<2, true, true, 0, kProbSplit>(sk + (b ^ 1) * kT, sv + b * kT, ra, lane, x.sc, sc, sn, mx,
                                         [&](auto n, int j) {
                                           constexpr int kGap = std::max(1, (decltype(n)::value * 5 / 8 - 2) / (2 * kC));
                                           if (j >= 2 && (j - 2) % kGap == 0 && (j - 2) / kGap < 2 * kC) copy((j - 2) / kGap);
@@ -428,7 +428,7 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
     ++it;
   }
   if (!active) return true;
-  w.template step<2, false, true, 0, true>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
+  w.template step<2, false, true, 0, kProbSplit>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
   const float lt = pair_sum(w.l);
   const int q = 32 * wave + (lane & 31), h = lane >> 5;
   if (q >= p.rows) return true;

@@ -145,6 +145,7 @@ struct Args {
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
   int narrow;                          // there may be pieces of a wave
+  int wide_cost;                       // time of a key to 128 rows, in times of one to few rows; 0: dealt as equal
   const uint16_t *q, *kp, *vp;
   const int32_t *tables, *lens, *ids, *shared;
   int32_t* count;
@@ -174,6 +175,7 @@ struct Plan {                          // LDS
 
 struct Cuts {
   int pieces[3];                       // of each kind, per key-value head (kNarrow: per four)
+  int worth;                           // pieces of few rows that take a group as long as one of many
 };
 
 __device__ __forceinline__ int up_to(int x, int y) { return (int)(((uint32_t)x + y - 1) / (uint32_t)y); }
@@ -369,10 +371,12 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
   const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), kMidKeys));
+  const int wide_chunk = max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys));
+  cut.worth = max(1, (wide_chunk * x.wide_cost + chunk / 2) / chunk);
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
-  cut_keys(leads ? pre : 0, wide ? max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys)) : chunk, 64, pre_n, pre_l);
+  cut_keys(leads ? pre : 0, wide ? wide_chunk : chunk, 64, pre_n, pre_l);
   const bool done = live && pre == 0 && own_n == 1;
   // Prefix sums: pieces of each kind, rows of results.
   const int own_all = own_n * own_tiles, pre_all = pre_n * pre_tiles;
@@ -478,6 +482,7 @@ plan_kernel(Args x) {
   make_plan<kPlan>(x, s, true, cut);
   const int all = min(cut.pieces[0] + cut.pieces[1] + cut.pieces[2], x.most);
   if (threadIdx.x < 3) x.count[threadIdx.x] = cut.pieces[threadIdx.x];
+  if (threadIdx.x == 3) x.count[3] = cut.worth;
   for (int k = threadIdx.x; k < all; k += kPlan) {
     int j = k;
     const int kind = kind_of(cut, j);
@@ -501,11 +506,21 @@ __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem)
   } else if (x.mode == kPlanned) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) cut.pieces[i] = x.count[i];
+    cut.worth = x.count[3];
   } else {
     cut.pieces[x.narrow ? kNarrow : kFewRows] = x.most;
   }
   const int64_t whole = (int64_t)(cut.pieces[kManyRows] + cut.pieces[kFewRows]) * kv, all = whole + (int64_t)cut.pieces[kNarrow] * fours;
-  const int64_t f = (int64_t)threadIdx.x * gridDim.x + (threadIdx.x % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  // Row r of the deal: the r-th piece of every group, but that a group which begins with a piece of many
+  // rows sits out the rows that this one is worth (as many as leave room for all pieces).
+  const int64_t groups = gridDim.x, many = (int64_t)cut.pieces[kManyRows] * kv;
+  const int worth = many == 0 || many >= groups ? 1 : (int)min((int64_t)max(cut.worth, 1), (kTodo * groups - (all - many)) / many);
+  const bool busy = blockIdx.x < many;
+  const int r = (int)threadIdx.x + (busy && threadIdx.x > 0 ? worth - 1 : 0);
+  const bool part = r > 0 && r < worth;             // only the other groups take part
+  const int64_t seat = part ? blockIdx.x - many : blockIdx.x, seats = part ? groups - many : groups;
+  const int64_t before = r == 0 ? 0 : r < worth ? groups + (r - 1) * (groups - many) : groups + (worth - 1) * (groups - many) + (r - worth) * groups;
+  const int64_t f = before + (r % 2 ? seats - 1 - seat : seat);
   if (threadIdx.x < kTodo && f < all) {
     const uint32_t at = (uint32_t)(f < whole ? f : f - whole), heads = f < whole ? kv : fours;
     int k = (int)(at / heads);
@@ -661,6 +676,7 @@ inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const voi
   x.key_bytes = key_bytes;
   x.mode = never_cut(c, a, shared != nullptr, x.tiles, x.key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   if (x.mode == kWhole) shared = nullptr;
+  x.wide_cost = 0;
   x.page_bits = __builtin_ctz(c.page);
   x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;

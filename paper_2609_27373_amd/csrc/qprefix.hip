@@ -23,14 +23,17 @@ namespace {
 //      a slice of the B operand as it stands; the lane loads the same four tokens at dims
 //      (D / 16) n .., widens a pair of dims of all eight keys, and two permutes a register make the A
 //      operands of two MFMAs, row m of the t-th being dim (D / 16) m + t
-// kAhead tiles are in flight in registers.
+// kTilesAhead tiles are in flight in registers.
 // ---------------------------------------------------------------------------
-constexpr int kAhead = 2;
+template <int D, int B, int NT>
+constexpr int kTilesAhead = NT == 2 && D * B > 384 ? 1 : 2;   // as many as registers hold
 
 template <int D, int B>
 struct Raw {                           // a lane's share of a tile of 32 keys
   uint32_t k[2][Kept<D, B>::kWords], v[2][Kept<D, B>::kWords];
   uint32_t ks[2][D == 96 ? 2 : 1], vs[2][D == 96 ? 2 : 1];
+  int64_t at[2];                       // bytes of a plane before the half's codes
+  int apart[2];                        // and from there to its scales
   bool ok[2];                          // the half has a page
 };
 
@@ -62,7 +65,7 @@ __device__ __forceinline__ int fresh_tid() {
 template <int D, int B, int NT, bool kAlone>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, float* lds) {
   using L = Kept<D, B>;
-  constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT, kWords = L::kWords;
+  constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT, kWords = L::kWords, kAhead = kTilesAhead<D, B, NT>;
   const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int rows = x.rows, page = x.c.page;
@@ -92,48 +95,43 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[u][t] = f32x4_t{};
   }
-  // Page ids of this wave's tiles: lane 2 i + s has the one of half s of tile i (mod 32), -1 for none.
+  // Where the halves of this wave's tiles lie in a plane: lane 2 i + s has the bytes before half s of tile i (mod 32), -1
+  // for no page.
   const int tiles = my_head < x.c.kv_heads ? (p.k1 - begin + stride - 1) / stride : 0;
-  int ids = -1;
+  const int page_bytes = page * (L::kRow + L::kScales);
+  int64_t halves = -1;
   auto load_ids = [&](int i0) {
     const int key = begin + stride * (i0 + (lane >> 1)) + 16 * (lane & 1);
-    ids = key < p.k1 ? table[key >> x.page_bits] : -1;
-    if (!in_range(ids, x.c.pages)) ids = -1;
+    const int id = key < p.k1 ? table[key >> x.page_bits] : -1;
+    halves = in_range(id, x.c.pages) ? ((int64_t)id * x.c.kv_heads + kh) * page_bytes + (key & (page - 1)) * L::kRow : -1;
   };
-  const int page_bytes = page * (L::kRow + L::kScales);
   const int k_code = (4 * n + g) * L::kPiece, v_code = lane * L::kPiece;
   const int k_scale = n * L::kScales + D / 4 * g / 32, k_last = n * L::kScales + (D / 4 * g + D / 4 - 8) / 32;
   const int v_scale = 4 * (g * L::kScales + D / 16 * n / 32), v_last = 4 * (g * L::kScales + (D / 16 * n + D / 16 - 2) / 32);
   const char *kp = (const char*)x.kp, *vp = (const char*)x.vp;
-  auto half = [&](int i, int s, bool& ok, size_t& scales) {   // bytes of a plane before the codes, the scales, of half s of tile i
-    const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + s);
-    const int t = (begin + stride * i + 16 * s) & (page - 1);
-    ok = id >= 0;
-    const size_t head = ((size_t)(ok ? id : 0) * x.c.kv_heads + kh) * page_bytes;
-    scales = head + page * L::kRow + t * L::kScales;
-    return head + t * L::kRow;
-  };
   Raw<D, B> raw[kAhead];
   auto load_k = [&](int i, Raw<D, B>& w) {
     if ((i & 31) == 0) load_ids(i);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      size_t scales;
-      const size_t codes = half(i, s, w.ok[s], scales);
-      load_words<kWords>(kp + codes + k_code, w.k[s]);
-      w.ks[s][0] = *(const uint8_t*)(kp + scales + k_scale);
-      if constexpr (D == 96) w.ks[s][1] = *(const uint8_t*)(kp + scales + k_last);
+      const int lo = __builtin_amdgcn_readlane((int)halves, 2 * (i & 31) + s), hi = __builtin_amdgcn_readlane((int)(halves >> 32), 2 * (i & 31) + s);
+      w.ok[s] = hi >= 0;
+      w.at[s] = w.ok[s] ? (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo) : 0;
+      // Of the page's scales, those of token t are (kRow - kScales) t bytes nearer than its codes.
+      w.apart[s] = page * L::kRow - ((begin + stride * i + 16 * s) & (page - 1)) * (L::kRow - L::kScales);
+      const char* codes = kp + w.at[s];
+      load_words<kWords>(codes + k_code, w.k[s]);
+      w.ks[s][0] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_scale));
+      if constexpr (D == 96) w.ks[s][1] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_last));
     }
   };
-  auto load_v = [&](int i, Raw<D, B>& w) {
+  auto load_v = [&](Raw<D, B>& w) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bool ok;
-      size_t scales;
-      const size_t codes = half(i, s, ok, scales);
-      load_words<kWords>(vp + codes + v_code, w.v[s]);
-      w.vs[s][0] = *(const uint32_t*)(vp + scales + v_scale);
-      if constexpr (D == 96) w.vs[s][1] = *(const uint32_t*)(vp + scales + v_last);
+      const char* codes = vp + w.at[s];
+      load_words<kWords>(codes + v_code, w.v[s]);
+      w.vs[s][0] = *(const uint32_t*)(codes + (uint32_t)(w.apart[s] + v_scale));
+      if constexpr (D == 96) w.vs[s][1] = *(const uint32_t*)(codes + (uint32_t)(w.apart[s] + v_last));
     }
   };
   // Past its last tile a wave loads what page 0 holds, which nothing uses.
@@ -141,7 +139,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       load_k(i, raw[i]);
-      load_v(i, raw[i]);
+      load_v(raw[i]);
     }
   }
   uint32_t poison = 0;                              // NaN values set aside
@@ -197,19 +195,23 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
         }
       }
     }
-    u32x4_t pb[NT], pr[NT];
+    uint32_t far = 0;                                 // a scale is past what fp16 holds
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < (D == 96 ? 2 : 1); ++j) far |= past_half<B>(w.vs[h][j]);
+    const bool half = __builtin_amdgcn_ballot_w64(far != 0) == 0;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      float mx = -INFINITY;
+      float mx = s[u][0][0];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[u][h][r]);
-      mx = quad_max(mx) * x.sc;
-      const bool grow = mx > m[u];
-      if (__builtin_amdgcn_ballot_w64(grow)) {
-        const float mn = grow ? mx : m[u];
-        const float alpha = mn == m[u] ? 1.f : fast_exp2(m[u] - mn);
+      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[u][r >> 2][r & 3]);
+      // The reference of the exponents is raised as kProbHalf says, not for each new maximum.
+      if (__builtin_amdgcn_ballot_w64(mx * x.sc > m[u] + kHalfTop)) {
+        mx = quad_max(mx) * x.sc;
+        const bool grow = mx > m[u] + kHalfTop;
+        const float mn = grow ? mx - kHalfLow : m[u];
+        const float alpha = grow ? fast_exp2(m[u] - mn) : 1.f;
         l[u] *= alpha;
 #pragma unroll
         for (int t = 0; t < kT; ++t)                 // in place, as in WaveRows::softmax
@@ -220,49 +222,65 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       const float mb = m[u] == -INFINITY ? 0.f : m[u];
       float ts = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float y[4];
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          y[r] = fast_exp2(__builtin_fmaf(s[u][h][r], x.sc, -mb));
-          ts += y[r];
+          s[u][h][r] = fast_exp2(__builtin_fmaf(s[u][h][r], x.sc, -mb));
+          ts += s[u][h][r];
         }
-        uint32_t rest[2];
-        pb[u][2 * h] = split_bf16x2(y[0], y[1], rest[0]);
-        pb[u][2 * h + 1] = split_bf16x2(y[2], y[3], rest[1]);
-        pr[u][2 * h] = rest[0];
-        pr[u][2 * h + 1] = rest[1];
-      }
       l[u] += ts;
     }
+    // Values in fp16 and probabilities with 11 bits where that is exact for the values, else both in bf16 and the
+    // probabilities as two numbers.
+    auto weigh = [&](auto in_half) {
+      constexpr bool kHalf = decltype(in_half)::value;
+      u32x4_t pb[NT], pr[NT];
 #pragma unroll
-    for (int b = 0; b < L::kPairs; ++b) {
-      uint32_t y[8];                                // the pair of dims of all keys
+      for (int u = 0; u < NT; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t word = w.vs[e >> 2][0];
-        uint32_t sw = word;
-        if constexpr (D == 96) {                    // pair 1 of piece 5 lies in the next scale
-          const uint32_t last = w.vs[e >> 2][1];
-          sw = b == 0 ? word : b == 2 || n == 5 ? last : word;
+        for (int j = 0; j < 4; ++j) {
+          const float y0 = s[u][j >> 1][2 * (j & 1)], y1 = s[u][j >> 1][2 * (j & 1) + 1];
+          if constexpr (kHalf) {
+            pb[u][j] = pack_f16x2(y0, y1);
+          } else {
+            uint32_t rest;
+            pb[u][j] = split_bf16x2(y0, y1, rest);
+            pr[u][j] = rest;
+          }
         }
-        y[e] = widen_at<B>(w.v[e >> 2], scale_of(sw, e & 3), (e & 3) * L::kPairs + b);
+#pragma unroll
+      for (int b = 0; b < L::kPairs; ++b) {
+        uint32_t y[8];                              // the pair of dims of all keys
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t sw = w.vs[e >> 2][0];
+          if constexpr (D == 96) sw = b == 2 || (b == 1 && n == 5) ? w.vs[e >> 2][1] : sw;   // pair 1 of piece 5 lies in the next scale
+          y[e] = widen_at<B, kHalf>(w.v[e >> 2], scale_of(sw, e & 3), (e & 3) * L::kPairs + b);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          u32x4_t f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], c ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) {
+            f32x4_t& to = o[u][2 * b + c];
+            if constexpr (kHalf) to = mfma16x16x32_f16(f, pb[u], to);
+            else to = mfma16x16x32(f, pr[u], mfma16x16x32(f, pb[u], to));
+          }
+        }
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        u32x4_t f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], c ? 0x07060302u : 0x05040100u);
-#pragma unroll
-        for (int u = 0; u < NT; ++u) o[u][2 * b + c] = mfma16x16x32(f, pr[u], mfma16x16x32(f, pb[u], o[u][2 * b + c]));
-      }
-    }
-    load_v(i + kAhead, w);
+    };
+    if (half) weigh(std::true_type{});
+    else weigh(std::false_type{});
+    load_v(w);
   };
   for (int i = 0; i < tiles; i += kAhead) {
-    tile(i, raw[0]);
-    if (i + 1 >= tiles) break;
-    tile(i + 1, raw[1]);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j >= tiles) break;
+      tile(i + j, raw[j]);
+    }
   }
   // Join the waves.
   float* mls = lds + 4 * kRows * kStride;
@@ -313,11 +331,186 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   }
 }
 
+// ---------------------------------------------------------------------------
+// A piece of up to 128 rows, all of which see all its keys (whole tiles of 64): the
+// pipeline of the dense kernel (WaveRows::step), four waves of 32 rows over rings of two K
+// and two V tiles in LDS, in bf16: a wave widens 16 consecutive keys of a tile, which lie in one page, for
+// all four, a tile ahead of their use, from registers that were loaded a step before.  False, with
+// nothing done, if some page id of the piece names no page.
+// ---------------------------------------------------------------------------
+template <int D, int B>
+__device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* smem) {
+  using L = Kept<D, B>;
+  using G = Geo<D>;
+  using S = Swizzle<D>;
+  constexpr int kT = S::kTile, kC = D / 32, kWords = L::kWords;
+  const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, n = lane & 15;
+  const int rows = x.rows, page = x.c.page, kh = p.head;
+  const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
+  const int tiles = (p.k1 - p.k0) / kKeyTile;
+  // Page ids of this wave's keys: lane i has the one of tile 64 u + i, of stretch u and the next one.
+  auto load_ids = [&](int u) {
+    const int key = p.k0 + (64 * u + lane) * kKeyTile + 16 * wave;
+    return key < p.k1 ? table[key >> x.page_bits] : 0;
+  };
+  int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
+  // All pages there, and all scales of values such that fp16 holds the values: those of four tokens a thread.
+  uint32_t bad = 0;
+  for (int t = p.k0 + 4 * tid; t < p.k1; t += 1024) {
+    const int id = table[t >> x.page_bits];
+    if (!in_range(id, x.c.pages)) {
+      bad = 1;
+      break;
+    }
+    const char* scales = (const char*)x.vp + ((size_t)id * x.c.kv_heads + kh) * (page * (L::kRow + L::kScales)) + page * L::kRow;
+#pragma unroll
+    for (int i = 0; i < L::kScales; ++i) bad |= past_half<B>(*(const uint32_t*)(scales + L::v_scale(t & (page - 1), i)));
+  }
+  if (__syncthreads_or(bad != 0)) return false;
+  WaveRows<D> w;
+  w.reset();
+  {
+    const int r = p.row0 + min(32 * wave + (lane & 31), p.rows - 1);
+    const int b = p.first + r / rows;
+    const uint16_t* row = x.q + (((size_t)b * x.c.kv_heads + kh) * rows + r % rows) * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
+  }
+  ReadAddr<D> ra;
+  ra.init(lane);
+  const int page_bytes = page * (L::kRow + L::kScales);
+  const int k_code = (4 * n + g) * L::kPiece, v_code = lane * L::kPiece;
+  const int k_scale = n * L::kScales + D / 4 * g / 32, k_last = n * L::kScales + (D / 4 * g + D / 4 - 8) / 32;
+  const int v_scale = 4 * (g * L::kScales + D / 16 * n / 32), v_last = 4 * (g * L::kScales + (D / 16 * n + D / 16 - 2) / 32);
+  uint32_t kw[kWords], vw[kWords], ks[2], vs[2];    // this wave's share of the tiles to be widened next
+  auto source = [&](const uint16_t* pool, int it, const char*& scales) {
+    const int id = __builtin_amdgcn_readlane(it >> 6 == stretch ? ids : next_ids, it & 63);
+    const int t = (p.k0 + it * kKeyTile + 16 * wave) & (page - 1);
+    const char* head = (const char*)pool + ((size_t)id * x.c.kv_heads + kh) * page_bytes;
+    scales = head + page * L::kRow + t * L::kScales;
+    return head + t * L::kRow;
+  };
+  auto load_k = [&](int it) {
+    const char* scales;
+    load_words<kWords>(source(x.kp, min(it, tiles - 1), scales) + k_code, kw);
+    ks[0] = *(const uint8_t*)(scales + k_scale);
+    if constexpr (D == 96) ks[1] = *(const uint8_t*)(scales + k_last);
+  };
+  auto load_v = [&](int it) {
+    const char* scales;
+    load_words<kWords>(source(x.vp, min(it, tiles - 1), scales) + v_code, vw);
+    vs[0] = *(const uint32_t*)(scales + v_scale);
+    if constexpr (D == 96) vs[1] = *(const uint32_t*)(scales + v_last);
+  };
+  // Eight dims of key n into the K tile; a token's dims into the V tile.
+  const int k_row = k_lds_row(16 * wave + n);
+  auto put_k = [&](char* tile, int e) {
+    const uint32_t byte = D != 96 || e == 0 ? ks[0] : e == 2 || g == 1 ? ks[D == 96] : ks[0];
+    u32x4_t f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = widen_at<B>(kw, scale_of(byte, 0), 4 * e + j);
+    *(u32x4_t*)(tile + k_row * S::kRow + S::k_chunk(k_row, kC * g + e) * 16) = f;
+  };
+  auto put_v = [&](char* tile, int e) {
+    const int row = 16 * wave + 4 * g + e, at = D / 8 * n;
+    uint32_t f[D / 32];
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      uint32_t sw = vs[0];
+      if constexpr (D == 96) sw = b == 2 || (b == 1 && n == 5) ? vs[1] : vs[0];
+      f[b] = widen_at<B, true>(vw, scale_of(sw, e), e * L::kPairs + b);
+    }
+    char* to = tile + row * S::kRow + S::v_block(row, at / 64) * 64 + at % 64;
+    if constexpr (D == 128) *(u32x4_t*)to = u32x4_t{f[0], f[1], f[2], f[3]};
+    else if constexpr (D == 64) *(u32x2_t*)to = u32x2_t{f[0], f[1]};
+    else
+#pragma unroll
+      for (int b = 0; b < 3; ++b) *(uint32_t*)(to + 4 * b) = f[b];
+  };
+  char *sk = smem, *sv = smem + 2 * kT;
+  auto put_all_k = [&](int it) {
+#pragma unroll
+    for (int e = 0; e < kC; ++e) put_k(sk + (it & 1) * kT, e);
+  };
+  load_k(0);
+  load_v(0);
+  put_all_k(0);
+  if (tiles > 1) {
+    load_k(1);
+    put_all_k(1);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) put_v(sv, e);
+  load_v(1);
+  load_k(2);
+  __syncthreads();
+  const bool active = 32 * wave < p.rows;
+  f32x16_t s0[2], s1[2];
+  float mx = 0.f;
+  if (active) w.template step<2, true, false, 0, kProbHalf>(sk, sv, ra, lane, x.sc, s1, s0, mx, [](auto, int) {}, [](f32x16_t*) {});
+  __syncthreads();                                  // K(0) read by every wave: K(2) may take its place
+  // Step `it`: S^T of tile it + 1, softmax and PV of tile it; V(it + 1) and K(it + 2)
+  // go where V(it - 1) and K(it) were, and the words of the ones after them are loaded.
+  auto fused = [&](int it, f32x16_t sc[2], f32x16_t sn[2]) {
+    const int b = it & 1;
+    if (it >> 6 != stretch) {
+      stretch = it >> 6;
+      ids = next_ids;
+      next_ids = load_ids(stretch + 1);
+    }
+    const bool more = it + 2 < tiles;
+    auto part = [&](int i) {                        // 4 + kC parts
+      if (i < 4) put_v(sv + (b ^ 1) * kT, i);
+      if (i == 3) load_v(it + 2);
+      if (i >= 4 && more) put_k(sk + b * kT, i - 4);
+      if (i == 3 + kC) load_k(it + 3);
+    };
+    if (active) {
+      w.template step<2, true, true, 0, kProbHalf>(sk + (b ^ 1) * kT, sv + b * kT, ra, lane, x.sc, sc, sn, mx,
+                                              [&](auto n, int j) {
+                                                constexpr int kGap = (decltype(n)::value - 2) / (4 + kC);
+                                                if (j >= 2 && (j - 2) % kGap == 0 && (j - 2) / kGap < 4 + kC) part((j - 2) / kGap);
+                                              },
+                                              [](f32x16_t*) {});
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4 + kC; ++i) part(i);
+    }
+    __syncthreads();
+  };
+  int it = 0;
+  for (; it + 2 < tiles; it += 2) {
+    fused(it, s0, s1);
+    fused(it + 1, s1, s0);
+  }
+  if (it + 1 < tiles) {
+    fused(it, s0, s1);
+    s0[0] = s1[0];
+    s0[1] = s1[1];
+    ++it;
+  }
+  if (!active) return true;
+  w.template step<2, false, true, 0, kProbHalf>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
+  const float lt = pair_sum(w.l);
+  const int q = 32 * wave + (lane & 31), h = lane >> 5;
+  if (q >= p.rows) return true;
+  const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + q;
+#pragma unroll
+  for (int t = 0; t < G::kDTiles; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(f32x4_t*)(x.part + at * D + 32 * t + 8 * j + 4 * h) =
+          f32x4_t{w.o[t][4 * j], w.o[t][4 * j + 1], w.o[t][4 * j + 2], w.o[t][4 * j + 3]};
+  if (h == 0) x.ml[at] = float2{w.m, lt};
+  return true;
+}
+
 template <int D, int B, int NT, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 qpiece_kernel(Args x) {
-  constexpr int kJoin = 4 * 16 * (kShared ? 2 : NT) * (D + 6) * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[kJoin];
+  constexpr int kJoin = 4 * 16 * (kShared ? 2 : NT) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
   __shared__ Piece todo[kTodo];
   const int count = my_pieces(x, todo, smem);
@@ -328,12 +521,14 @@ qpiece_kernel(Args x) {
     for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
     if (i > 0) __syncthreads();                     // the piece before has left the LDS
     if (kShared && p.see == kSeeAll) {
-      Piece s = p;
+      if (p.kind == kManyRows && tile_piece<D, B>(x, p, smem)) continue;
+      Piece s = p;                                  // a few rows, or, where a page is missing, many a few at a time
       for (int r = 0; r < p.rows; r += 32) {
         if (r > 0) __syncthreads();
         s.row0 = p.row0 + r;
         s.rows = min(32, p.rows - r);
-        stream_piece<D, B, 2, false>(x, s, (float*)smem);
+        if (s.rows <= 16) stream_piece<D, B, 1, false>(x, s, (float*)smem);
+        else stream_piece<D, B, 2, false>(x, s, (float*)smem);
       }
     } else if (p.kind == kNarrow) {
       stream_piece<D, B, NT, true>(x, p, (float*)smem);
@@ -369,7 +564,8 @@ size_t qprefix_workspace_bytes(const Cache& c, const Queries& a) { return space_
 hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void* q, const void* kp, const void* vp,
                           const int32_t* tables, const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse,
                           void* ws, hipStream_t st) {
-  const Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
+  Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
+  x.wide_cost = 3;
   const auto run = [&](auto d, auto b) {
     constexpr int D = decltype(d)::value, B = decltype(b)::value;
     return x.tile == 16 ? launch<D, B, 1>(x, st) : launch<D, B, 2>(x, st);

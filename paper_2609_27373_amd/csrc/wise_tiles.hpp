@@ -133,6 +133,14 @@ __device__ __forceinline__ int score_key(int t, int r, int h) {
   return 32 * t + 16 * (j >> 1) + 8 * h + 4 * (j & 1) + i;
 }
 
+// How probabilities enter the product with V: in bf16, as two bf16 numbers (16 bits, an MFMA
+// more), or in fp16 beside a V in fp16 (11 bits).  fp16 has 15 binades above 1 and 14 below before it
+// loses bits: a row's reference m is then kept kHalfLow below its largest score and raised only when a score is
+// kHalfTop above it, so that what rounds to a subnormal weighs less than 2^-20 of the row's largest, and no
+// probability passes 2^14.  The sums of a row then lie up to 2^14 higher.
+enum { kProbBf16, kProbSplit, kProbHalf };
+constexpr float kHalfLow = 6.f, kHalfTop = 14.f;
+
 // ---------------------------------------------------------------------------
 // Per-wave state and steps of the tile engine.
 // ---------------------------------------------------------------------------
@@ -297,11 +305,13 @@ struct WaveRows {
   }
 
   // New running max from a tile's max mx; true (wave-uniform) when some
-  // query's max grew: alpha then holds the factor of O, l is rescaled here.
+  // query's max grew: alpha then holds the factor of O, l is rescaled here.  kLow: m lies kHalfLow
+  // below a tile's max, and is raised only where that is past kHalfTop above it.
+  template <bool kLow = false>
   __device__ __forceinline__ bool raise_max(float mx, float& alpha) {
-    const bool grow = mx > m;
+    const bool grow = mx > (kLow ? m + kHalfTop : m);
     if (!__builtin_amdgcn_ballot_w64(grow)) return false;
-    const float mn = grow ? mx : m;
+    const float mn = grow ? (kLow ? mx - kHalfLow : mx) : m;
     alpha = (mn == m) ? 1.f : fast_exp2(m - mn);
     l *= alpha;
     m = mn;
@@ -320,9 +330,9 @@ struct WaveRows {
   // step leave nothing else to fill a wave's waits; mid(n, j) runs in slot j
   // (the copies).  The wave's priority falls through the step, so of the two
   // waves of a SIMD the one behind issues first and they reach the barrier
-  // together.  VALU and matrix cores are then both close to full.  kSplit: PV with 16
-  // bits of each probability, in two MFMAs a slot.
-  template <int H, bool kQk, bool kPv, int kParts, bool kSplit = false, class Mid, class Mask>
+  // together.  VALU and matrix cores are then both close to full.  kProb: how
+  // probabilities enter PV.
+  template <int H, bool kQk, bool kPv, int kParts, int kProb = kProbBf16, class Mid, class Mask>
   __device__ __forceinline__ void step(const char* kn, const char* vt, const ReadAddr<D>& ra, int lane, float c,
                                        f32x16_t s[H], f32x16_t sn[H], float& mx, Mid mid, Mask maskn) {
     constexpr int kN = G::kDChunks * H;          // MFMAs of S^T; PV has as many
@@ -358,11 +368,13 @@ struct WaveRows {
       a += pv[2 * k];
       a += pv[2 * k + 1];
       uint32_t w;
-      if constexpr (kSplit) {
+      if constexpr (kProb == kProbSplit) {
         uint32_t rest;
         w = split_bf16x2(pv[2 * k], pv[2 * k + 1], rest);
         asm volatile("" : "+v"(rest));
         pr[2 * t + (r >> 3)][(r & 7) >> 1] = rest;
+      } else if constexpr (kProb == kProbHalf) {
+        w = pack_f16x2(pv[2 * k], pv[2 * k + 1]);
       } else {
         w = pack_bf16x2(pv[2 * k], pv[2 * k + 1]);
       }
@@ -398,7 +410,7 @@ struct WaveRows {
       if constexpr (kPv) {
         if (j == kS0) {
           __builtin_amdgcn_sched_barrier(0);
-          grew = raise_max(mx, alpha);
+          grew = raise_max<kProb == kProbHalf>(mx, alpha);
           mb = (m == -INFINITY) ? 0.f : m;
         }
 #pragma unroll
@@ -433,8 +445,9 @@ struct WaveRows {
       if constexpr (kPv) {
         const int i = j - kN;
         if (i + kAhead < kN) read_v(i + kAhead);
-        o[i % G::kDTiles] = mfma32x32x16(vf[i], pb[i / G::kDTiles], o[i % G::kDTiles]);
-        if constexpr (kSplit) o[i % G::kDTiles] = mfma32x32x16(vf[i], pr[i / G::kDTiles], o[i % G::kDTiles]);
+        if constexpr (kProb == kProbHalf) o[i % G::kDTiles] = mfma32x32x16_f16(vf[i], pb[i / G::kDTiles], o[i % G::kDTiles]);
+        else o[i % G::kDTiles] = mfma32x32x16(vf[i], pb[i / G::kDTiles], o[i % G::kDTiles]);
+        if constexpr (kProb == kProbSplit) o[i % G::kDTiles] = mfma32x32x16(vf[i], pr[i / G::kDTiles], o[i % G::kDTiles]);
 #pragma unroll
         for (int k = 0; k < kPairs; ++k)
           if (k >= pairs_before(j) && k < pairs_before(j + 1)) pair_exp(k);

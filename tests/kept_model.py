@@ -17,7 +17,7 @@ def magnitudes(bits):
 
 
 def quantise(x, bits):
-    """(codes [..., d], scale bytes [..., d / 32]) of x [..., d]: the nearest code by searching through all of them."""
+    """(codes [..., d], scale bytes [..., d / 32]) of x [..., d]: the nearest code."""
     x = np.asarray(x, dtype=np.float64)
     y = x.reshape(*x.shape[:-1], -1, 32)
     bad = ~np.isfinite(y).all(-1)
@@ -29,14 +29,10 @@ def quantise(x, bits):
         e = np.where(a > TOP[bits] * 2.0 ** (k - 1), k, e)
     table = magnitudes(bits)[:8 if bits == 4 else 127]
     z = np.abs(y) / 2.0 ** e[..., None].astype(float)
-    flat = z.reshape(-1)
-    codes = np.empty(flat.shape, dtype=np.int64)
-    for i in range(0, flat.size, 1 << 16):
-        off = np.abs(flat[i:i + (1 << 16), None] - table)
-        near = off == off.min(-1, keepdims=True)
-        even = near & (np.arange(len(table)) % 2 == 0)
-        codes[i:i + (1 << 16)] = np.where(even.any(-1), even.argmax(-1), near.argmax(-1))
-    codes = codes.reshape(z.shape) | (np.signbit(y).astype(np.int64) << (bits - 1))
+    middle = (table[1:] + table[:-1]) / 2            # between codes i and i + 1; on it, the even one of the two
+    low, high = np.searchsorted(middle, z, "left"), np.searchsorted(middle, z, "right")
+    codes = np.where(low % 2 == 0, low, high)
+    codes = codes | (np.signbit(y).astype(np.int64) << (bits - 1))
     codes = np.where(bad[..., None], 0, codes)
     return codes.reshape(x.shape).astype(np.uint8), np.where(bad, 255, e + 127).astype(np.uint8)
 
@@ -99,14 +95,15 @@ def read_pool(pool, page, d, bits):
 
 
 def attend(q, k_pool, v_pool, tables, lens, ids, page, scale):
-    """(o, lse, bound, lse_bound) in fp64, as cache_model.attend, with the bounds that 16-bit probabilities allow.
+    """(o, lse, bound, lse_bound) in fp64, as cache_model.attend, with the bounds that 11-bit probabilities allow.
 
-    o is rounded to bf16: half a step, 2^-8 |o|.  A probability enters the product with V as two bf16 numbers, which
-    leaves 2^-8 of what the first left, 2^-8 of it: 2^-16 A, A = sum p |v|.  A score is an fp32 sum of d exact products, off by
-    at most E = scale d 2^-24 max sum |q k| (its own rounding and the scale's, 2^-23 of |s|, in it for d >= 64), which
+    o is rounded to bf16: half a step, 2^-8 |o|.  A probability enters the product with V in fp16 (or as two bf16 numbers, which
+    leaves less): half a step, 2^-12 of it, so 2^-12 A in all, A = sum p |v|; where the row's reference makes it a subnormal, it is off
+    by at most 2^-25 while the row's largest is 2^6 or more, which is 2^-31 of z: n 2^-31 max |v|.  A score is an fp32 sum of d exact
+    products, off by at most E = scale d 2^-24 max sum |q k| (its own rounding and the scale's, 2^-23 of |s|, in it for d >= 64), which
     changes a probability and the sum by e^E each; the exponentials, and rescaled partial sums over n keys, one
-    fp32 rounding of each product's sum: 2^-18 + n 2^-24.  Below the normal numbers a probability, taken against the
-    row's largest (so that z >= 1), and either of its two parts may become 0: 2^-126 each, 2^-125 sum |v| in all; so may o: 2^-126."""
+    fp32 rounding of each product's sum: 2^-18 + n 2^-24.  Below fp32's normal numbers a probability, taken against the
+    row's largest (so that z >= 1), and either of two parts may become 0: 2^-126 each, 2^-125 sum |v| in all; so may o: 2^-126."""
     batch, heads, q_len, d = q.shape
     pages, kv = k_pool.shape[:2]
     gq = heads // kv
@@ -135,7 +132,8 @@ def attend(q, k_pool, v_pool, tables, lens, ids, page, scale):
                 o[b, hs, t] = p @ vv
                 lse[b, hs, t] = (top + np.log(z))[:, 0]
                 e = scale * d * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T).max(-1)
-                extra = 2.0 ** -16 + 2 * e + 2.0 ** -18 + m.sum() * 2.0 ** -24
-                bound[b, hs, t] = 2.0 ** -8 * np.abs(o[b, hs, t]) + (1 + 2.0 ** -8) * extra[:, None] * (p @ np.abs(vv)) + 2.0 ** -125 * np.abs(vv).sum(0) + 2.0 ** -126
+                extra = 2.0 ** -12 + 2 * e + 2.0 ** -18 + m.sum() * 2.0 ** -24
+                small = m.sum() * 2.0 ** -31 * np.abs(vv).max(0) + 2.0 ** -125 * np.abs(vv).sum(0) + 2.0 ** -126
+                bound[b, hs, t] = 2.0 ** -8 * np.abs(o[b, hs, t]) + (1 + 2.0 ** -8) * (extra[:, None] * (p @ np.abs(vv)) + small)
                 lse_bound[b, hs, t] = e + 2.0 ** -18 + m.sum() * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse[b, hs, t])
     return o, lse, bound, lse_bound
