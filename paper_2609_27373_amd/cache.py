@@ -38,6 +38,8 @@ _I32, _BF16, _F32 = torch.int32, torch.bfloat16, torch.float32
 # The current stream's handle.  torch's public call builds a Stream object for it (1.2 us of the 7 of a call);
 # its own generated code asks for the handle alone.
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# The current device, which torch's public call first makes sure there is (as the cache's tensors have).
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class PagedCache:
@@ -59,7 +61,7 @@ class PagedCache:
         self._lens = self._own(lens, (seqs,), _I32, "lens", lambda s: torch.zeros(s, **i32))
         self._refs = self._own(refs, (pages,), _I32, "refs", lambda s: torch.zeros(s, **i32))
         self.device = self._pool.device
-        self._index = self.device.index
+        self._index, self._ordinal = self.device.index, self._pool.get_device()
         for t, name in ((self._tables, "tables"), (self._lens, "lens"), (self._refs, "refs")):
             if t.device != self.device:
                 raise ValueError(f"{name} is on {t.device}, the pool on {self.device}")
@@ -69,6 +71,9 @@ class PagedCache:
         # The buffers above, checked once and for all, as the C calls take them.
         self._state = tuple(t.data_ptr() for t in (self._tables, self._lens, self._refs))
         self._ws = (self._workspace.data_ptr(), n)
+        plane = self._pool.numel() // self.shape.planes * self._pool.element_size()
+        self._heads = (kv_heads, head_dim)
+        self._planes = [(at, at + plane) for at in range(self._pool.data_ptr(), self._pool.data_ptr() + 2 * layers * plane, 2 * plane)]
 
     pool = property(lambda self: self._pool, doc="bf16 [2 * layers][pages][kv_heads][page][head_dim]")
     tables = property(lambda self: self._tables, doc="int32 [seqs][max_pages]")
@@ -100,10 +105,10 @@ class PagedCache:
         """The address of a call's tensor, or None."""
         if t is None:
             return None
-        if t.dtype is not dtype or t.device != self.device or not t.is_contiguous() or t.numel() < numel:
-            raise ValueError(f"{name} must be contiguous {dtype} on {self.device} of at least {numel} elements, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
-        return t.data_ptr()
+        if t.dtype is dtype and t.get_device() == self._ordinal and t.is_contiguous() and t.numel() >= numel:
+            return t.data_ptr()
+        raise ValueError(f"{name} must be contiguous {dtype} on {self.device} of at least {numel} elements, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
     def _call(self, fn, *args):
         index = self._index
@@ -111,7 +116,7 @@ class PagedCache:
             raise ValueError("the cache is not on a GPU")
         entry = getattr(wise.load(), fn)
         stream = _stream(index)
-        if torch.cuda.current_device() == index:
+        if _current() == index:
             status = entry(self._c, *args, stream)
         else:
             with torch.cuda.device(index):
@@ -149,19 +154,17 @@ class PagedCache:
 
     def _rows(self, layer, k, v, seq_ids, counts, n):
         """Addresses of a layer's planes, and of the arguments that name rows of keys and values."""
-        c = self.shape
-        if k.dim() != 4 or k.shape[0] != n or k.shape[1] != c.kv_heads or k.shape[3] != c.head_dim or v.shape != k.shape:
-            raise ValueError(f"k and v must be [{n}][{c.kv_heads}][tokens][{c.head_dim}], got {tuple(k.shape)}, {tuple(v.shape)}")
-        rows = k.numel()
+        shape = tuple(k.shape)
+        if len(shape) != 4 or shape[0] != n or (shape[1], shape[3]) != self._heads or v.shape != shape:
+            c = self.shape
+            raise ValueError(f"k and v must be [{n}][{c.kv_heads}][tokens][{c.head_dim}], got {shape}, {tuple(v.shape)}")
         return (*self._layer(layer), self._arg(seq_ids, _I32, "seq_ids", n), self._arg(counts, _I32, "counts", n),
-                self._arg(k, _BF16, "k", rows), self._arg(v, _BF16, "v", rows))
+                self._arg(k, _BF16, "k", 0), self._arg(v, _BF16, "v", 0))
 
     def _layer(self, layer):
-        if not 0 <= layer < self.shape.planes // 2:
-            raise ValueError(f"layer {layer} of {self.shape.planes // 2}")
-        plane = self._pool.numel() // self.shape.planes * self._pool.element_size()
-        at = self._pool.data_ptr() + 2 * layer * plane
-        return at, at + plane
+        if not 0 <= layer < len(self._planes):
+            raise ValueError(f"layer {layer} of {len(self._planes)}")
+        return self._planes[layer]
 
     def layer(self, layer):
         """The planes of one layer: (keys, values), each as the pool without its first dimension."""

@@ -145,6 +145,7 @@ struct Args {
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
   int narrow;                          // there may be pieces of a wave
+  int shares;                          // even shares per key-value head; 0: none
   int wide_cost;                       // time of a key to 128 rows, in times of one to few rows; 0: dealt as equal
   const uint16_t *q, *kp, *vp;
   const int32_t *tables, *lens, *ids, *shared;
@@ -219,6 +220,34 @@ __device__ __forceinline__ int plan_all(int v, int none, Op op, int32_t* waves) 
   return v;
 }
 
+// Even shares, instead of pieces of about the same length.  Per key-value head, the segments of a batch are laid one behind
+// another, each kPieceKeys longer than its keys (what a piece costs beside them), and cut into x.shares equal stretches, one a
+// work-group: it does what lies in its stretch, and all end together (32 sequences of up to 8K in 1144 pieces over 512
+// groups ended 19 to 41 us after the start, 32 on average).  A cut inside a segment is moved to a multiple of 128 keys.
+constexpr int kPieceKeys = 256, kShareSeqs = 256, kShareLeast = 1024;
+
+struct Shares {                        // LDS
+  int32_t at[kShareSeqs], pre[kShareSeqs], len[kShareSeqs], id[kShareSeqs], members[kShareSeqs], pre_slot[kShareSeqs], own_slot[kShareSeqs];
+  int32_t size, used;                  // of a stretch; how many there are, 0: pieces are made in the other way
+  int32_t stretch, first;              // where the group is: of the stretches of all heads, and the sequence in it, -1 for the start
+};
+
+// Keys of a segment of `keys` keys at `at` that lie before stretch j.
+__device__ __forceinline__ int share_cut(int at, int keys, int j, int size) {
+  const int64_t y = (int64_t)j * size - at - kPieceKeys;
+  return y >= keys ? keys : y <= 0 ? 0 : min(keys, ((int)y + 64) & ~127);
+}
+// The first stretch that has keys of it, and how many have.
+__device__ __forceinline__ int share_first(int at, int keys, int size) {
+  const int j = (int)((uint32_t)(at + kPieceKeys) / (uint32_t)size);
+  return j + (share_cut(at, keys, j + 1, size) == 0);
+}
+__device__ __forceinline__ int share_count(int at, int keys, int size) {
+  if (keys <= 0) return 0;
+  const int last = (int)((uint32_t)(at + kPieceKeys + keys - 1) / (uint32_t)size);
+  return last - (share_cut(at, keys, last, size) >= keys) - share_first(at, keys, size) + 1;
+}
+
 // Cuts runs where neighbours differ in what they share: `keys` are the keys that
 // a sequence could read together with the one before it (0: none).  A run of n that
 // reads m keys once saves (n - 1) m reads, and m is the least `keys` inside it, so one
@@ -283,9 +312,10 @@ __device__ __forceinline__ int split_runs(Plan<kN>& s, bool live, int keys) {
   }
 }
 
-// Runs and pieces of all sequences.  Writes x.joint if `write`.
+// Runs and pieces of all sequences, or (shares, where there is a place for them and they do better) even shares.
+// Writes x.joint if `write`.
 template <int kN>
-__device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
+__device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut, Shares* shares = nullptr) {
   const int b = threadIdx.x, lane = b & 63, wave = kN > 64 ? b >> 6 : 0;
   const Cache& c = x.c;
   const Queries& a = x.a;
@@ -366,6 +396,61 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut) {
       k0 += s.wave_keys[w][0];
       k1 += s.wave_keys[w][1];
     }
+  }
+  if (shares != nullptr) {
+    // Where sequences are long, and segments one row tile each.
+    bool place = x.shares > 0 && k1 == 0 && k0 < (int64_t)1 << 29 && k0 >= (int64_t)a.batch * kShareLeast;
+    if (place) {
+      const bool odd = leads && pre_tiles > 1;
+      place = !(kN > 64 ? __syncthreads_or(odd) : __builtin_amdgcn_ballot_w64(odd) != 0);
+    }
+    if (place) {
+      const int mine = (leads ? pre + kPieceKeys : 0) + (live && own > 0 ? own + kPieceKeys : 0);
+      int end = wave_scan_add(mine), total = __builtin_amdgcn_readlane(end, 63);
+      if constexpr (kN > 64) {
+        if (lane == 63) s.wave_sum[wave][0] = end;
+        __syncthreads();
+        total = 0;
+        for (int w = 0; w < kN / 64; ++w) {
+          const int y = s.wave_sum[w][0];
+          end += w < wave ? y : 0;
+          total += y;
+        }
+        __syncthreads();
+      }
+      const int size = max(up_to(total, x.shares), kPieceKeys + kFewKeys), at = end - mine;
+      const int pre_n = leads ? share_count(at, pre, size) : 0, own_n = live ? share_count(end - own - kPieceKeys, own, size) : 0;
+      const bool done = live && pre == 0 && own_n == 1;
+      const int slots = (done ? 0 : own_n * c.kv_heads * rows) + pre_n * c.kv_heads * pre_rows;
+      int slot = wave_scan_add(slots);
+      if constexpr (kN > 64) {
+        if (lane == 63) s.wave_sum[wave][1] = slot;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) slot += s.wave_sum[w][1];
+      }
+      slot -= slots;
+      shares->at[b] = at;
+      for (int i = b + kN; i < kShareSeqs; i += kN) shares->at[i] = 0x7fffffff;
+      shares->pre[b] = pre;
+      shares->len[b] = len;
+      shares->id[b] = id;
+      shares->members[b] = leads ? n : 0;
+      shares->pre_slot[b] = slot;
+      shares->own_slot[b] = done ? -1 : slot + pre_n * c.kv_heads * pre_rows;
+      s.pre_slot[b] = slot;
+      s.pre_pieces[b] = pre_n;
+      if (b == 0) {
+        shares->size = size;
+        shares->used = up_to(total, size);
+        shares->stretch = blockIdx.x;
+        shares->first = -1;
+      }
+      plan_sync<kN>();
+      if (write && live)
+        x.joint[b] = Joint{s.pre_slot[start], pre > 0 ? s.pre_pieces[start] : 0, n * rows, (b - start) * rows, shares->own_slot[b], own_n, done, 0};
+      return;
+    }
+    if (b == 0) shares->used = 0;
   }
   auto even = [&](int64_t sum, int groups, int least) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
@@ -496,13 +581,18 @@ plan_kernel(Args x) {
 // groups that began with the lightest.
 constexpr int kTodo = 8;
 
-__device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem) {
+template <int kTodo>
+__device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem, Shares* shares = nullptr) {
   const int kv = x.c.kv_heads, fours = (kv + 3) / 4;
   Cuts cut{};
   const bool one_wave = x.a.batch <= 64;
   if (x.mode == kOwnPlan) {
-    if (!one_wave) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, cut);
-    else if (threadIdx.x < 64) make_plan<64>(x, *(Plan<64>*)smem, blockIdx.x == 0, cut);
+    if (!one_wave) make_plan<256>(x, *(Plan<256>*)smem, blockIdx.x == 0, cut, shares);
+    else if (threadIdx.x < 64) make_plan<64>(x, *(Plan<64>*)smem, blockIdx.x == 0, cut, shares);
+    if (shares != nullptr) {
+      __syncthreads();
+      if (shares->used > 0) return 0;
+    }
   } else if (x.mode == kPlanned) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) cut.pieces[i] = x.count[i];
@@ -551,6 +641,50 @@ __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem)
     todo[threadIdx.x] = p;
   }
   return __syncthreads_count(threadIdx.x < kTodo && f < all);
+}
+
+// The next pieces of this group's stretches: two (of shared pages, of its own) for each of kTodo / 2 sequences, those
+// without keys of 0 rows.  False if there are none left.
+template <int kTodo>
+__device__ __forceinline__ bool share_pieces(const Args& x, Shares& s, Piece* todo) {
+  __syncthreads();                                  // the list before is done with
+  const int size = s.size, kv = x.c.kv_heads, j = s.stretch / kv, head = s.stretch - j * kv;
+  if (j >= s.used) return false;
+  const int first = s.first >= 0 ? s.first : plan_entry<kShareSeqs>(s.at, j * size), next = first + kTodo / 2;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool inside = next < x.a.batch && s.at[next] < (int64_t)(j + 1) * size;
+    s.first = inside ? next : -1;
+    s.stretch += inside ? 0 : gridDim.x;
+  }
+  if (threadIdx.x < kTodo) {
+    const int e = first + (int)threadIdx.x / 2;
+    Piece p;
+    p.rows = 0;
+    if (e < x.a.batch && s.at[e] < (int64_t)(j + 1) * size) {
+      const bool shared = threadIdx.x % 2 == 0;
+      const int lead = s.members[e] > 0 ? s.pre[e] + kPieceKeys : 0;
+      const int at = s.at[e] + (shared ? 0 : lead), keys = shared ? (lead > 0 ? s.pre[e] : 0) : s.len[e] - s.pre[e];
+      const int k0 = share_cut(at, keys, j, size), k1 = share_cut(at, keys, j + 1, size);
+      if (k0 < k1) {
+        const int i = j - share_first(at, keys, size);
+        p.first = e;
+        p.table = s.id[e];
+        p.row0 = 0;
+        p.rows = p.seg_rows = shared ? s.members[e] * x.rows : x.rows;
+        p.k0 = shared ? k0 : s.pre[e] + k0;
+        p.k1 = shared ? k1 : s.pre[e] + k1;
+        p.see = shared ? kSeeAll : s.len[e] - x.a.q_len + 1;
+        p.slot = shared ? s.pre_slot[e] + i * kv * p.rows : s.own_slot[e] < 0 ? -1 : s.own_slot[e] + i * kv * p.rows;
+        p.kind = kFewRows;
+        p.head = head;
+        p.pad = 0;
+      }
+    }
+    todo[threadIdx.x] = p;
+  }
+  __syncthreads();
+  return true;
 }
 
 // ---------------------------------------------------------------------------
@@ -676,7 +810,7 @@ inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const voi
   x.key_bytes = key_bytes;
   x.mode = never_cut(c, a, shared != nullptr, x.tiles, x.key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   if (x.mode == kWhole) shared = nullptr;
-  x.wide_cost = 0;
+  x.wide_cost = x.shares = 0;
   x.page_bits = __builtin_ctz(c.page);
   x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;

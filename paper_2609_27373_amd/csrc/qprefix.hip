@@ -506,35 +506,47 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
   return true;
 }
 
+constexpr int kMine = 16;              // pieces of a group, at most: no more groups than the chip holds at once, even where pieces are many
+
 template <int D, int B, int NT, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 qpiece_kernel(Args x) {
   constexpr int kJoin = 4 * 16 * (kShared ? 2 : NT) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
-  __shared__ Piece todo[kTodo];
-  const int count = my_pieces(x, todo, smem);
-  for (int i = 0; i < count; ++i) {
-    Piece p = todo[i];
-    int32_t* w = (int32_t*)&p;                     // the same in every lane
-#pragma unroll
-    for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
-    if (i > 0) __syncthreads();                     // the piece before has left the LDS
-    if (kShared && p.see == kSeeAll) {
-      if (p.kind == kManyRows && tile_piece<D, B>(x, p, smem)) continue;
-      Piece s = p;                                  // a few rows, or, where a page is missing, many a few at a time
-      for (int r = 0; r < p.rows; r += 32) {
-        if (r > 0) __syncthreads();
-        s.row0 = p.row0 + r;
-        s.rows = min(32, p.rows - r);
-        if (s.rows <= 16) stream_piece<D, B, 1, false>(x, s, (float*)smem);
-        else stream_piece<D, B, 2, false>(x, s, (float*)smem);
-      }
-    } else if (p.kind == kNarrow) {
-      stream_piece<D, B, NT, true>(x, p, (float*)smem);
-    } else {
-      stream_piece<D, B, NT, false>(x, p, (float*)smem);
+  __shared__ Piece todo[kMine];
+  __shared__ Shares shares;
+  int count = my_pieces<kMine>(x, todo, smem, &shares);
+  const bool even = x.mode == kOwnPlan && __builtin_amdgcn_readfirstlane(shares.used) > 0;
+  for (;;) {
+    if (even) {
+      if (!share_pieces<kMine>(x, shares, todo)) return;
+      count = kMine;
     }
+    for (int i = 0; i < count; ++i) {
+      Piece p = todo[i];
+      int32_t* w = (int32_t*)&p;                   // the same in every lane
+#pragma unroll
+      for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
+      if (p.rows == 0) continue;
+      if (i > 0) __syncthreads();                   // the piece before has left the LDS
+      if (kShared && p.see == kSeeAll) {
+        if (p.kind == kManyRows && tile_piece<D, B>(x, p, smem)) continue;
+        Piece s = p;                                // a few rows, or many a few at a time, where tile_piece did not
+        for (int r = 0; r < p.rows; r += 32) {
+          if (r > 0) __syncthreads();
+          s.row0 = p.row0 + r;
+          s.rows = min(32, p.rows - r);
+          if (s.rows <= 16) stream_piece<D, B, 1, false>(x, s, (float*)smem);
+          else stream_piece<D, B, 2, false>(x, s, (float*)smem);
+        }
+      } else if (p.kind == kNarrow) {
+        stream_piece<D, B, NT, true>(x, p, (float*)smem);
+      } else {
+        stream_piece<D, B, NT, false>(x, p, (float*)smem);
+      }
+    }
+    if (!even) return;
   }
 }
 
@@ -547,7 +559,7 @@ hipError_t launch(const Args& x, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = kHold;
-  const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kTodo - 1) / kTodo));
+  const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kMine - 1) / kMine));
   if (x.shared != nullptr) qpiece_kernel<D, B, NT, true><<<grid, 256, 0, st>>>(x);
   else qpiece_kernel<D, B, NT, false><<<grid, 256, 0, st>>>(x);
   const hipError_t e = hipGetLastError();
@@ -566,6 +578,15 @@ hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void
                           void* ws, hipStream_t st) {
   Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
   x.wide_cost = 3;
+  // As many shares a head as give most groups one, or some number of times as many where that comes out evener.
+  if (x.tiles == 1 && x.mode == kOwnPlan) {
+    double best = 1e9;
+    for (int turns = 1; turns <= 2; ++turns) {
+      const int n = std::max(1, kHold * turns / c.kv_heads);
+      const double cost = (double)((n * (int64_t)c.kv_heads + kHold - 1) / kHold) / n * (1 + 0.1 * turns);
+      if (cost < best) best = cost, x.shares = n;
+    }
+  }
   const auto run = [&](auto d, auto b) {
     constexpr int D = decltype(d)::value, B = decltype(b)::value;
     return x.tile == 16 ? launch<D, B, 1>(x, st) : launch<D, B, 2>(x, st);
