@@ -62,6 +62,14 @@ __device__ __forceinline__ int fresh_tid() {
   return tid;
 }
 
+// The kernel's argument where the hardware has put it, unknown to the compiler, which would else keep what it has read of it,
+// for every kind of piece at once, and spill scalars inside their loops.
+__device__ __forceinline__ const Args& fresh_args() {
+  auto p = (const __attribute__((address_space(4))) Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Args*)p;
+}
+
 template <int D, int B, int NT, bool kAlone>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, float* lds) {
   using L = Kept<D, B>;
@@ -530,20 +538,18 @@ qpiece_kernel(Args x) {
       for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
       if (p.rows == 0) continue;
       if (i > 0) __syncthreads();                   // the piece before has left the LDS
-      if (kShared && p.see == kSeeAll) {
-        if (p.kind == kManyRows && tile_piece<D, B>(x, p, smem)) continue;
-        Piece s = p;                                // a few rows, or many a few at a time, where tile_piece did not
-        for (int r = 0; r < p.rows; r += 32) {
-          if (r > 0) __syncthreads();
-          s.row0 = p.row0 + r;
-          s.rows = min(32, p.rows - r);
-          if (s.rows <= 16) stream_piece<D, B, 1, false>(x, s, (float*)smem);
-          else stream_piece<D, B, 2, false>(x, s, (float*)smem);
-        }
-      } else if (p.kind == kNarrow) {
-        stream_piece<D, B, NT, true>(x, p, (float*)smem);
-      } else {
-        stream_piece<D, B, NT, false>(x, p, (float*)smem);
+      if (kShared && p.kind == kManyRows && tile_piece<D, B>(fresh_args(), p, smem)) continue;
+      if (p.kind == kNarrow) {
+        stream_piece<D, B, NT, true>(fresh_args(), p, (float*)smem);
+        continue;
+      }
+      Piece s = p;                                  // of shared pages it may have more rows: 32 at a time
+      for (int r = 0; r < p.rows; r += 32) {
+        if (r > 0) __syncthreads();
+        s.row0 = p.row0 + r;
+        s.rows = min(32, p.rows - r);
+        if (NT == 2 || (kShared && s.rows > 16)) stream_piece<D, B, 2, false>(fresh_args(), s, (float*)smem);
+        else stream_piece<D, B, 1, false>(fresh_args(), s, (float*)smem);
       }
     }
     if (!even) return;
