@@ -80,24 +80,24 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return (t >> 7) * 255u;
 }
 
-// N words at p, which is aligned as a lane's bytes are.
-template <int N>
+// N words at p, which is aligned as a lane's bytes are.  kOnce: they are not read again soon, and need not stay in the L2.
+template <int N, bool kOnce = false>
 __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
   typedef uint32_t W2 __attribute__((ext_vector_type(2), aligned(8)));
   typedef uint32_t W3 __attribute__((ext_vector_type(3), aligned(4)));
   typedef uint32_t W4 __attribute__((ext_vector_type(4), aligned(8)));
   static_assert(N == 2 || N == 3 || N == 4 || N == 6 || N == 8, "words of a lane");
   if constexpr (N >= 4) {
-    const W4 x = *(const W4*)p;
+    const W4 x = kOnce ? __builtin_nontemporal_load((const W4*)p) : *(const W4*)p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = x[i];
-    if constexpr (N > 4) load_words<N - 4>(p + 16, w + 4);
+    if constexpr (N > 4) load_words<N - 4, kOnce>(p + 16, w + 4);
   } else if constexpr (N == 3) {
-    const W3 x = *(const W3*)p;
+    const W3 x = kOnce ? __builtin_nontemporal_load((const W3*)p) : *(const W3*)p;
 #pragma unroll
     for (int i = 0; i < 3; ++i) w[i] = x[i];
   } else {
-    const W2 x = *(const W2*)p;
+    const W2 x = kOnce ? __builtin_nontemporal_load((const W2*)p) : *(const W2*)p;
     w[0] = x[0], w[1] = x[1];
   }
 }

@@ -145,6 +145,7 @@ struct Args {
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
   int narrow;                          // there may be pieces of a wave
+  int mid_keys, wide_fill, wide_keys;  // kMidKeys, kWideFill, kWideKeys, or what does better
   int shares;                          // even shares per key-value head; 0: none
   int wide_cost;                       // time of a key to 128 rows, in times of one to few rows; 0: dealt as equal
   const uint16_t *q, *kp, *vp;
@@ -455,8 +456,8 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut, Sha
   auto even = [&](int64_t sum, int groups, int least) {
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
-  const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), kMidKeys));
-  const int wide_chunk = max(even(k1, kWideGroups, kWideLeast), min(even(k1, kWideFill, kWideLeast), kWideKeys));
+  const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), x.mid_keys));
+  const int wide_chunk = max(even(k1, kWideGroups, kWideLeast), min(even(k1, x.wide_fill, kWideLeast), x.wide_keys));
   cut.worth = max(1, (wide_chunk * x.wide_cost + chunk / 2) / chunk);
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
@@ -811,6 +812,7 @@ inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const voi
   x.mode = never_cut(c, a, shared != nullptr, x.tiles, x.key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   if (x.mode == kWhole) shared = nullptr;
   x.wide_cost = x.shares = 0;
+  x.mid_keys = kMidKeys, x.wide_fill = kWideFill, x.wide_keys = kWideKeys;
   x.page_bits = __builtin_ctz(c.page);
   x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;

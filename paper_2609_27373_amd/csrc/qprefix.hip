@@ -70,10 +70,12 @@ __device__ __forceinline__ const Args& fresh_args() {
   return *(const Args*)p;
 }
 
-template <int D, int B, int NT, bool kAlone>
+template <int D, int B, int R, bool kAlone>
 __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, float* lds) {
   using L = Kept<D, B>;
-  constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT, kWords = L::kWords, kAhead = kTilesAhead<D, B, NT>;
+  constexpr int NT = (R + 15) / 16;
+  constexpr bool kPack = R == 8;
+  constexpr int kC = D / 32, kT = D / 16, kStride = D + 4, kRows = 16 * NT, kS = kPack ? 4 : 8, kWords = L::kWords, kAhead = kTilesAhead<D, B, NT>;
   const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
   const int rows = x.rows, page = x.c.page;
@@ -86,7 +88,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   int see[NT];
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
-    const int r = p.row0 + min(16 * u + n, p.rows - 1);
+    const int r = p.row0 + min(kPack ? n & 7 : 16 * u + n, p.rows - 1);
     const int b = p.first + r / rows, w = r % rows;
     see[u] = min(p.see + w % x.a.q_len, p.k1);
     const uint16_t* row = x.q + (((size_t)b * x.c.kv_heads + kh) * rows + w) * D + D / 4 * g;
@@ -128,7 +130,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       // Of the page's scales, those of token t are (kRow - kScales) t bytes nearer than its codes.
       w.apart[s] = page * L::kRow - ((begin + stride * i + 16 * s) & (page - 1)) * (L::kRow - L::kScales);
       const char* codes = kp + w.at[s];
-      load_words<kWords>(codes + k_code, w.k[s]);
+      load_words<kWords, B == 4>(codes + k_code, w.k[s]);
       w.ks[s][0] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_scale));
       if constexpr (D == 96) w.ks[s][1] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_last));
     }
@@ -173,14 +175,20 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       }
     }
     load_k(i + kAhead, w);
+    // kPack: the half of the columns that repeats the queries takes the scores of the second 16 keys.
+    float y[NT][kS];
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int r = 0; r < kS; ++r) y[u][r] = kPack ? (n < 8 ? s[u][0][r] : s[u][1][r]) : s[u][r >> 2][r & 3];
     if (masked) {
 #pragma unroll
       for (int u = 0; u < NT; ++u)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (key0 + 16 * h + 4 * g + r >= see[u] || !(h ? ok1 : ok0)) s[u][h][r] = -INFINITY;
+        for (int r = 0; r < kS; ++r) {
+          const bool second = kPack ? n >= 8 : r >= 4;
+          if (key0 + (second ? 16 : 0) + 4 * g + (r & 3) >= see[u] || !(second ? ok1 : ok0)) y[u][r] = -INFINITY;
+        }
       // Values that no row sees may be anything, and NaN must not reach the rows that don't see
       // it (0 * NaN is NaN): they count as 0 or as some number, and the rows that see NaN get it at the end.
 #pragma unroll
@@ -211,11 +219,12 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
     const bool half = __builtin_amdgcn_ballot_w64(far != 0) == 0;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      float mx = s[u][0][0];
+      float mx = y[u][0];
 #pragma unroll
-      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[u][r >> 2][r & 3]);
+      for (int r = 1; r < kS; ++r) mx = fmaxf(mx, y[u][r]);
       // The reference of the exponents is raised as kProbHalf says, not for each new maximum.
       if (__builtin_amdgcn_ballot_w64(mx * x.sc > m[u] + kHalfTop)) {
+        if constexpr (kPack) mx = fmaxf(mx, dpp_mov<0x128>(mx));   // row_ror 8
         mx = quad_max(mx) * x.sc;
         const bool grow = mx > m[u] + kHalfTop;
         const float mn = grow ? mx - kHalfLow : m[u];
@@ -230,12 +239,10 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       const float mb = m[u] == -INFINITY ? 0.f : m[u];
       float ts = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[u][h][r] = fast_exp2(__builtin_fmaf(s[u][h][r], x.sc, -mb));
-          ts += s[u][h][r];
-        }
+      for (int r = 0; r < kS; ++r) {
+        y[u][r] = fast_exp2(__builtin_fmaf(y[u][r], x.sc, -mb));
+        ts += y[u][r];
+      }
       l[u] += ts;
     }
     // Values in fp16 and probabilities with 11 bits where that is exact for the values, else both in bf16 and the
@@ -246,30 +253,31 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
       for (int u = 0; u < NT; ++u)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float y0 = s[u][j >> 1][2 * (j & 1)], y1 = s[u][j >> 1][2 * (j & 1) + 1];
+        for (int j = 0; j < kS / 2; ++j) {
           if constexpr (kHalf) {
-            pb[u][j] = pack_f16x2(y0, y1);
+            pb[u][j] = pack_f16x2(y[u][2 * j], y[u][2 * j + 1]);
           } else {
             uint32_t rest;
-            pb[u][j] = split_bf16x2(y0, y1, rest);
+            pb[u][j] = split_bf16x2(y[u][2 * j], y[u][2 * j + 1], rest);
             pr[u][j] = rest;
+            if constexpr (kPack) pr[u][2 + j] = (uint32_t)__builtin_amdgcn_mov_dpp((int)rest, 0x128, 0xF, 0xF, true);
           }
+          if constexpr (kPack) pb[u][2 + j] = (uint32_t)__builtin_amdgcn_mov_dpp((int)pb[u][j], 0x128, 0xF, 0xF, true);
         }
 #pragma unroll
       for (int b = 0; b < L::kPairs; ++b) {
-        uint32_t y[8];                              // the pair of dims of all keys
+        uint32_t v[8];                              // the pair of dims of all keys
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           uint32_t sw = w.vs[e >> 2][0];
           if constexpr (D == 96) sw = b == 2 || (b == 1 && n == 5) ? w.vs[e >> 2][1] : sw;   // pair 1 of piece 5 lies in the next scale
-          y[e] = widen_at<B, kHalf>(w.v[e >> 2], scale_of(sw, e & 3), (e & 3) * L::kPairs + b);
+          v[e] = widen_at<B, kHalf>(w.v[e >> 2], scale_of(sw, e & 3), (e & 3) * L::kPairs + b);
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           u32x4_t f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], c ? 0x07060302u : 0x05040100u);
+          for (int j = 0; j < 4; ++j) f[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], c ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int u = 0; u < NT; ++u) {
             f32x4_t& to = o[u][2 * b + c];
@@ -295,7 +303,8 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   const bool poisoned = __syncthreads_or(poison != 0);
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
-    const float lt = quad_sum(l[u]);
+    float lt = quad_sum(l[u]);
+    if constexpr (kPack) lt += dpp_mov<0x128>(lt);
     const int r = wave * kRows + 16 * u + n;
     if (g == 0) {
       mls[2 * r] = m[u];
@@ -516,10 +525,10 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
 
 constexpr int kMine = 16;              // pieces of a group, at most: no more groups than the chip holds at once, even where pieces are many
 
-template <int D, int B, int NT, bool kShared>
+template <int D, int B, int R, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 qpiece_kernel(Args x) {
-  constexpr int kJoin = 4 * 16 * (kShared ? 2 : NT) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
+  constexpr int kJoin = 4 * 16 * (kShared || R == 32 ? 2 : 1) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
   __shared__ Piece todo[kMine];
@@ -540,7 +549,7 @@ qpiece_kernel(Args x) {
       if (i > 0) __syncthreads();                   // the piece before has left the LDS
       if (kShared && p.kind == kManyRows && tile_piece<D, B>(fresh_args(), p, smem)) continue;
       if (p.kind == kNarrow) {
-        stream_piece<D, B, NT, true>(fresh_args(), p, (float*)smem);
+        stream_piece<D, B, R, true>(fresh_args(), p, (float*)smem);
         continue;
       }
       Piece s = p;                                  // of shared pages it may have more rows: 32 at a time
@@ -548,15 +557,15 @@ qpiece_kernel(Args x) {
         if (r > 0) __syncthreads();
         s.row0 = p.row0 + r;
         s.rows = min(32, p.rows - r);
-        if (NT == 2 || (kShared && s.rows > 16)) stream_piece<D, B, 2, false>(fresh_args(), s, (float*)smem);
-        else stream_piece<D, B, 1, false>(fresh_args(), s, (float*)smem);
+        if (R == 32 || (kShared && s.rows > R)) stream_piece<D, B, 32, false>(fresh_args(), s, (float*)smem);
+        else stream_piece<D, B, R == 8 ? 8 : 16, false>(fresh_args(), s, (float*)smem);
       }
     }
     if (!even) return;
   }
 }
 
-template <int D, int B, int NT>
+template <int D, int B, int R>
 hipError_t launch(const Args& x, hipStream_t st) {
   const int64_t rows = (int64_t)x.a.batch * x.a.heads * x.a.q_len;
   if (x.mode == kPlanned) {
@@ -566,8 +575,8 @@ hipError_t launch(const Args& x, hipStream_t st) {
   }
   const int64_t pieces = (int64_t)x.most * x.c.kv_heads, hold = kHold;
   const unsigned grid = (unsigned)std::min(pieces, std::max(hold, (pieces + kMine - 1) / kMine));
-  if (x.shared != nullptr) qpiece_kernel<D, B, NT, true><<<grid, 256, 0, st>>>(x);
-  else qpiece_kernel<D, B, NT, false><<<grid, 256, 0, st>>>(x);
+  if (x.shared != nullptr) qpiece_kernel<D, B, R, true><<<grid, 256, 0, st>>>(x);
+  else qpiece_kernel<D, B, R, false><<<grid, 256, 0, st>>>(x);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || x.mode == kWhole) return e;
   if (rows <= kFewJoins) join_kernel<D, 4><<<(unsigned)rows, 256, 0, st>>>(x, rows);
@@ -584,6 +593,7 @@ hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void
                           void* ws, hipStream_t st) {
   Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
   x.wide_cost = 3;
+  x.mid_keys = 1024, x.wide_fill = 256, x.wide_keys = 512;
   // As many shares a head as give most groups one, or some number of times as many where that comes out evener.
   if (x.tiles == 1 && x.mode == kOwnPlan) {
     double best = 1e9;
@@ -595,7 +605,7 @@ hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void
   }
   const auto run = [&](auto d, auto b) {
     constexpr int D = decltype(d)::value, B = decltype(b)::value;
-    return x.tile == 16 ? launch<D, B, 1>(x, st) : launch<D, B, 2>(x, st);
+    return x.rows <= 8 ? launch<D, B, 8>(x, st) : x.tile == 16 ? launch<D, B, 16>(x, st) : launch<D, B, 32>(x, st);
   };
   const auto by_dim = [&](auto b) {
     return c.head_dim == 64   ? run(std::integral_constant<int, 64>{}, b)

@@ -185,6 +185,22 @@ def test_long(gpu_lib, d, kv, gq, bits):
 
 
 @WIDTHS
+@pytest.mark.parametrize("page,d,kv,gq,q_len", [(16, 64, 2, 4, 1), (128, 128, 3, 1, 1), (32, 96, 1, 8, 2), (64, 128, 11, 1, 1)])
+@pytest.mark.parametrize("groups", [[(0, [1500, None, 2500, 900, 33, 4000])], [(40, [700, 1, 2100]), (0, [1900, 1300]), (70, [20, 1000, 9])],
+                                    [(0, [1200 + 7 * i for i in range(70)])]])
+def test_even_shares(gpu_lib, page, d, kv, gq, q_len, groups, bits):
+    """Sequences of more than 1024 tokens on average, which are laid one behind another and cut evenly: shared pages too, more
+    than 64 sequences, numbers of heads that the work-groups do not divide."""
+    if kv == 11 and len(groups[0][1]) > 10:
+        groups = [(0, groups[0][1][:9])]
+    groups = [(pre * 16 // page, tails) for pre, tails in groups]
+    b = Batch(groups, page, d, kv, gq, bits, q_len, seed=page)
+    truth = b.truth()
+    for shared in (True, False):
+        b.check(*b.run(shared), truth)
+
+
+@WIDTHS
 @pytest.mark.parametrize("gain,scale", [(60.0, 0.0), (1.0, 3.0), (0.0, 0.0), (1.0, 1e-6)])
 def test_scores(gpu_lib, gain, scale, bits):
     """Scores so large that one key has all the weight, none at all, and a scale of the caller's."""
