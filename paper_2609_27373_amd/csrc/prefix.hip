@@ -464,7 +464,8 @@ piece_kernel(Args x) {
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
   __shared__ Piece todo[kTodo];
-  const int count = my_pieces<kTodo>(x, todo, smem);
+  __shared__ int listed;
+  const int count = my_pieces<kTodo>(x, todo, &listed, smem);
   for (int i = 0; i < count; ++i) {
     Piece p = todo[i];
     int32_t* w = (int32_t*)&p;                     // the same in every lane

@@ -145,7 +145,7 @@ struct Args {
   int mode;                            // kWhole, kOwnPlan or kPlanned
   int most;                            // pieces that the workspace holds
   int narrow;                          // there may be pieces of a wave
-  int mid_keys, wide_fill, wide_keys;  // kMidKeys, kWideFill, kWideKeys, or what does better
+  int mid_keys, fill_all, wide_keys;   // kMidKeys, kWideGroups instead of kWideFill, kWideKeys, or what does better
   int shares;                          // even shares per key-value head; 0: none
   int wide_cost;                       // time of a key to 128 rows, in times of one to few rows; 0: dealt as equal
   const uint16_t *q, *kp, *vp;
@@ -457,8 +457,12 @@ __device__ void make_plan(const Args& x, Plan<kN>& s, bool write, Cuts& cut, Sha
     return (int)min(max((sum * c.kv_heads + groups - 1) / groups, (int64_t)least), (int64_t)1 << 30);
   };
   const int chunk = max(even(k0, kGroups, kFewKeys), min(even(k0, kGroups / 2, kFewKeys), x.mid_keys));
-  const int wide_chunk = max(even(k1, kWideGroups, kWideLeast), min(even(k1, x.wide_fill, kWideLeast), x.wide_keys));
-  cut.worth = max(1, (wide_chunk * x.wide_cost + chunk / 2) / chunk);
+  int wide_chunk = kWideLeast;
+  cut.worth = 1;
+  if (k1 > 0) {
+    wide_chunk = max(even(k1, kWideGroups, kWideLeast), min(x.fill_all ? even(k1, kWideGroups, kWideLeast) : even(k1, kWideFill, kWideLeast), x.wide_keys));
+    cut.worth = max(1, (int)((float)wide_chunk * (float)x.wide_cost / (float)chunk + 0.5f));
+  }
   const bool narrow = x.narrow && own <= kNarrowKeys;
   int own_n, own_l, pre_n, pre_l;
   cut_keys(live ? own : 0, chunk, 32, own_n, own_l);
@@ -583,7 +587,7 @@ plan_kernel(Args x) {
 constexpr int kTodo = 8;
 
 template <int kTodo>
-__device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem, Shares* shares = nullptr) {
+__device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, int* listed, char* smem, Shares* shares = nullptr) {
   const int kv = x.c.kv_heads, fours = (kv + 3) / 4;
   Cuts cut{};
   const bool one_wave = x.a.batch <= 64;
@@ -605,7 +609,7 @@ __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem,
   // Row r of the deal: the r-th piece of every group, but that a group which begins with a piece of many
   // rows sits out the rows that this one is worth (as many as leave room for all pieces).
   const int64_t groups = gridDim.x, many = (int64_t)cut.pieces[kManyRows] * kv;
-  const int worth = many == 0 || many >= groups ? 1 : (int)min((int64_t)max(cut.worth, 1), (kTodo * groups - (all - many)) / many);
+  const int worth = many == 0 || many >= groups ? 1 : min(max(cut.worth, 1), max(1, (int)min((float)(kTodo * groups - (all - many)) / (float)many * 0.9999f, 1e6f)));
   const bool busy = blockIdx.x < many;
   const int r = (int)threadIdx.x + (busy && threadIdx.x > 0 ? worth - 1 : 0);
   const bool part = r > 0 && r < worth;             // only the other groups take part
@@ -641,7 +645,13 @@ __device__ __forceinline__ int my_pieces(const Args& x, Piece* todo, char* smem,
     p.head = head;
     todo[threadIdx.x] = p;
   }
-  return __syncthreads_count(threadIdx.x < kTodo && f < all);
+  // The first wave has them all.
+  if (threadIdx.x < 64) {
+    const int mine = __popcll(__builtin_amdgcn_ballot_w64(threadIdx.x < kTodo && f < all));
+    if (threadIdx.x == 0) *listed = mine;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(*listed);
 }
 
 // The next pieces of this group's stretches: two (of shared pages, of its own) for each of kTodo / 2 sequences, those
@@ -812,7 +822,7 @@ inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const voi
   x.mode = never_cut(c, a, shared != nullptr, x.tiles, x.key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   if (x.mode == kWhole) shared = nullptr;
   x.wide_cost = x.shares = 0;
-  x.mid_keys = kMidKeys, x.wide_fill = kWideFill, x.wide_keys = kWideKeys;
+  x.mid_keys = kMidKeys, x.fill_all = 0, x.wide_keys = kWideKeys;
   x.page_bits = __builtin_ctz(c.page);
   x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;

@@ -532,8 +532,9 @@ qpiece_kernel(Args x) {
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
   __shared__ Piece todo[kMine];
+  __shared__ int listed;
   __shared__ Shares shares;
-  int count = my_pieces<kMine>(x, todo, smem, &shares);
+  int count = my_pieces<kMine>(x, todo, &listed, smem, &shares);
   const bool even = x.mode == kOwnPlan && __builtin_amdgcn_readfirstlane(shares.used) > 0;
   for (;;) {
     if (even) {
@@ -593,7 +594,7 @@ hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void
                           void* ws, hipStream_t st) {
   Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
   x.wide_cost = 3;
-  x.mid_keys = 1024, x.wide_fill = 256, x.wide_keys = 512;
+  x.mid_keys = 1024, x.fill_all = 1, x.wide_keys = 512;
   // As many shares a head as give most groups one, or some number of times as many where that comes out evener.
   if (x.tiles == 1 && x.mode == kOwnPlan) {
     double best = 1e9;
