@@ -633,7 +633,7 @@ size_t wise_qcache_page_bytes(const wise_cache* c, int32_t bits);
  *
  * Of the 32 dims of a scale, with a their largest magnitude: e is the least whole
  * number with a <= T 2^e, where T = 7 for 4 bits and 464 for 8 (so that a itself is off by at most
- * half a step), within -125..125 for 4 bits and -117..119 for 8; a value
+ * half a step), within -125..125 for 4 bits and -117..119 for 8, and 0 where a = 0; a value
  * x becomes the code nearest to x / 2^e, of two that are equally near the even one, the
  * largest if x / 2^e is past it.  Where one of the 32 is infinite or NaN, all 32 are kept as NaN.
  *
@@ -679,10 +679,12 @@ wise_status wise_qcache_compact(const wise_cache* c, int32_t bits,
                                 size_t workspace_bytes, void* hip_stream);
 
 /*
- * wise_qcache_attn — wise_prefix_attn over what such pages hold: the queries,
- * the sums and the probabilities are as exact as there, only the keys and values are
- * those that were kept.  A NaN value makes its dim NaN in every row that
+ * wise_qcache_attn — wise_prefix_attn over what such pages hold: the keys and values are
+ * those that were kept, as exact as they are there.  A NaN value makes its dim NaN in every row that
  * sees it, whatever its weight, and in no other; a NaN key the whole row.
+ * Probabilities enter the product with V with 11 bits (where scales of values are outside 2^-23..2^8,
+ * for 8 bits 2^-15..2^7, with 16).  Sums take up to 14 binades of fp32's range: values of 2^112 and
+ * more may give infinities.
  *
  *   workspace : wise_qcache_workspace_bytes(c, bits, a) bytes, 256-byte aligned.
  * The others, and the errors, as for wise_prefix_attn (WISE_ERR_UNSUPPORTED

@@ -62,10 +62,11 @@ __device__ __forceinline__ uint32_t widen_at(const uint32_t* w, float scale, int
 }
 
 // Nonzero bits where one of a word's scales makes products that fp16 does not hold exactly: it does
-// with e from -23 to 8 for 4 bits (0.5 to 6 times 2^e), from -15 to 0 (of what would do to 7) for 8 (2^-9 to 448).
+// with e from -23 to 8 for 4 bits (0.5 to 6 times 2^e, and would to 13), from -15 to 7 for 8 (2^-9 to 448).  A byte
+// carries into the next one only where it is itself past a border.
 template <int B>
 __device__ __forceinline__ uint32_t past_half(uint32_t w) {
-  return B == 4 ? ((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u : (w ^ 0x70707070u) & 0xf0f0f0f0u;
+  return B == 4 ? ((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u : ~((w + 0x10101010u) & (w + 0x79797979u)) & 0x80808080u;
 }
 
 // Scale byte i of a word, as widen_pair takes it.

@@ -29,11 +29,12 @@ __device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
 }
 
 // Scale byte for a largest magnitude of the given bits: e from a <= T 2^e, within the exponents that
-// leave every product of a code and the scale normal in bf16; 255 if the bits are of an infinite value or NaN.
+// leave every product of a code and the scale normal in bf16; 255 if the bits are of an infinite value or NaN.  Zeros
+// take 2^0: the least scale would send the attention that reads them the longer way.
 template <int B>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
   const int e = B == 4 ? (((int)a + 31) >> 7) - 2 : (((int)a + 23) >> 7) - 8;
-  return a >= 0x7f80 ? 255 : B == 4 ? min(max(e, 2), 252) : min(max(e, 10), 246);
+  return a >= 0x7f80 ? 255 : a == 0 ? 127 : B == 4 ? min(max(e, 2), 252) : min(max(e, 10), 246);
 }
 
 // A lane's share of a token: D / 16 consecutive dims.
@@ -170,7 +171,11 @@ __device__ __forceinline__ int64_t page_of(const Cache& c, const int32_t* tables
 
 // ---------------------------------------------------------------------------
 // Append, and the way back.  16 lanes take the tokens of one entry and head that lie in one four of
-// positions, K and V: the unit in which values are laid out.
+// positions, K and V: the unit in which values are laid out, so a store of four tokens' values, as of each key, is
+// consecutive in the lanes, and a lane has up to eight loads of 16 bytes in flight.  A maximum over 32 dims is two or
+// three steps over the lanes.  Bound by HBM: 8 prompts of up to 4K tokens, 6 layers of 8 heads of 128 in 4 bits, 1285 MB
+// written and read back in 274 us (4.7 TB/s, the rate of a large copy); 32 histories of up to 8K read, 670 MB in
+// 133 us (5.0 TB/s).  Few tokens: 3.3 us on the device, 8 from Python.
 // ---------------------------------------------------------------------------
 struct Four {                          // the lanes' share of the work
   uint32_t entry, head;

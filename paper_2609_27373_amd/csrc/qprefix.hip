@@ -4,9 +4,12 @@
 // join are those of the cache in bf16 (prefix_plan.hpp); here is a piece of work.
 //
 // What is kept is exact in bf16 (a code has at most 4 significant bits, the scale is a
-// power of two), so each value is widened to bf16 in a register, two an instruction, right before
-// the matrix cores take it, and nothing else is rounded that the cache in bf16 does
-// not round: o, and the probabilities, which enter the product with V with 16 bits.
+// power of two), so each key is widened to bf16 in a register, two values an instruction, right before
+// the matrix cores take it, and a score is as exact as with keys in bf16.  Values are widened to fp16 where that
+// is exact too, which their scales tell (past_half), and meet probabilities of 11 bits in one MFMA: o is off by
+// 2^-12 of sum p |v| at most beside its own rounding of 2^-8, and measures 0.16 to 0.17% rms from its definition as
+// with exact probabilities.  Else both are bf16 and a probability is two numbers (split_bf16x2), an MFMA more.  One
+// number instead of two everywhere took 32 x 8K tokens from 45 to 44 us, 128 over a 32K document from 203 to 171.
 #include "kept.hpp"
 #include "prefix_plan.hpp"
 
@@ -14,7 +17,7 @@ namespace wise {
 namespace {
 
 // ---------------------------------------------------------------------------
-// A piece of up to 16 NT rows.  A wave takes every fourth tile of 32 keys (S^T = K Q^T and
+// A piece of up to R rows (8, 16, 32).  A wave takes every fourth tile of 32 keys (S^T = K Q^T and
 // O^T = V^T P^T in 16x16x32 MFMAs, queries in columns).  The sums may run in
 // any order, which the layout uses twice:
 //   K  lane (n, g), g = lane / 16, loads the quarter g of key n's dims, D / 4 of
@@ -23,10 +26,18 @@ namespace {
 //      a slice of the B operand as it stands; the lane loads the same four tokens at dims
 //      (D / 16) n .., widens a pair of dims of all eight keys, and two permutes a register make the A
 //      operands of two MFMAs, row m of the t-th being dim (D / 16) m + t
-// kTilesAhead tiles are in flight in registers.
+// Of up to 8 rows the 16 columns hold each twice, and the second half of the columns does the softmax of the second 16
+// keys: half the exponentials (1%).  kTilesAhead tiles are in flight in registers; a third one, or more waves than
+// two a SIMD, did no better (one of 128K tokens: 44 us with two, 45 with three, 46 with four).
+// Bound by HBM while tiles run, 1.05 us a tile of 32 keys of 128 in 4 bits with 2048 waves at work (8.5 TB/s, part of it from
+// the last-level cache).  A call has 10 to 15 us beside that: launch, plan (2 to 4), a piece's page ids and first
+// tiles (3.5), its join (1), the join of pieces (5).
+// Keys in 4 bits are loaded past the L2 (32 x 8K 39.8 -> 37.4 us, 128 x up to 4K 68.7 -> 65.2); in 8 bits a lane's bytes take
+// two loads that meet a line twice (128 x up to 4K 111 -> 120), and values past it lose where the last-level cache holds
+// a call's (8 samples of 4K 27 -> 29).
 // ---------------------------------------------------------------------------
 template <int D, int B, int NT>
-constexpr int kTilesAhead = NT == 2 && D * B > 384 ? 1 : 2;   // as many as registers hold
+constexpr int kTilesAhead = NT == 2 && D * B > 384 ? 1 : 2;   // registers hold no more in tiles of 32 rows
 
 template <int D, int B>
 struct Raw {                           // a lane's share of a tile of 32 keys
@@ -352,8 +363,10 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 // A piece of up to 128 rows, all of which see all its keys (whole tiles of 64): the
 // pipeline of the dense kernel (WaveRows::step), four waves of 32 rows over rings of two K
 // and two V tiles in LDS, in bf16: a wave widens 16 consecutive keys of a tile, which lie in one page, for
-// all four, a tile ahead of their use, from registers that were loaded a step before.  False, with
-// nothing done, if some page id of the piece names no page.
+// all four, a tile ahead of their use, from registers that were loaded a step before.  Bound by the exponentials and the
+// latency of two waves a SIMD: 1.5 us a tile of 64 keys of 128 alone on a CU, 2.1 beside a group of few rows (512 rows over
+// 32K tokens 108 us, 147 when 32 rows at a time were streamed).  False, with nothing done, if some page id of the piece names
+// no page, or a scale of its values is past what fp16 holds.
 // ---------------------------------------------------------------------------
 template <int D, int B>
 __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* smem) {
@@ -523,7 +536,9 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
   return true;
 }
 
-constexpr int kMine = 16;              // pieces of a group, at most: no more groups than the chip holds at once, even where pieces are many
+// Pieces of a group, at most: with 8 some calls had more groups than the chip holds at once, which planned in a second turn (64
+// samples at 4 layers of 55 heads: 283 us a step, 260).
+constexpr int kMine = 16;
 
 template <int D, int B, int R, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
@@ -593,9 +608,12 @@ hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void
                           const int32_t* tables, const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse,
                           void* ws, hipStream_t st) {
   Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
+  // Pieces are shorter work than in bf16, those of many rows the least so: a key to 128 rows takes three times one to few (128
+  // over a 32K document 170 us dealt as equal, 159 as once, 145 as twice or more often), pieces of few rows may be longer, those of
+  // many shorter (document 143 -> 137, 16 x 5 drafts 26.2 -> 25.7).
   x.wide_cost = 3;
   x.mid_keys = 1024, x.fill_all = 1, x.wide_keys = 512;
-  // As many shares a head as give most groups one, or some number of times as many where that comes out evener.
+  // As many shares a head as give each group one, or two where that comes out evener.
   if (x.tiles == 1 && x.mode == kOwnPlan) {
     double best = 1e9;
     for (int turns = 1; turns <= 2; ++turns) {

@@ -516,7 +516,7 @@ const char* wise_status_string(wise_status st) {
              "misaligned pointer";
     case WISE_ERR_UNSUPPORTED:
       return "WISE_ERR_UNSUPPORTED: head_dim must be 64/96/128, block 16/32/64/128, "
-             "seq_len/block <= 1024 for selection";
+             "seq_len/block <= 1024 for selection, bits of a cache 4/8";
     case WISE_ERR_RANGE: return "WISE_ERR_RANGE: tau outside (0, 1], bad scale or unknown flag bits";
     case WISE_ERR_WORKSPACE: return "WISE_ERR_WORKSPACE: workspace smaller than required";
     case WISE_ERR_HIP: return "WISE_ERR_HIP: a kernel launch failed";

@@ -27,6 +27,7 @@ def quantise(x, bits):
     e = np.full(a.shape, lo)
     for k in range(lo + 1, hi + 1):                  # the least e that is enough, or the largest there is
         e = np.where(a > TOP[bits] * 2.0 ** (k - 1), k, e)
+    e = np.where(a == 0, 0, e)
     table = magnitudes(bits)[:8 if bits == 4 else 127]
     z = np.abs(y) / 2.0 ** e[..., None].astype(float)
     middle = (table[1:] + table[:-1]) / 2            # between codes i and i + 1; on it, the even one of the two
