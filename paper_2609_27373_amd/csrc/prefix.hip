@@ -25,6 +25,30 @@
 namespace wise {
 namespace {
 
+// Whether every sequence is one piece, shared pages or not, which saves the plan and the
+// join.  By the tokens of a table (what a sequence can hold) and the groups G that this gives:
+//   up to 512: always, nothing shared.  1 x 301 tokens, 8 heads of 64: 12 -> 7.5 us; 1024 sequences of
+//     512 tokens, 8 heads of 128: 194 -> 161.  Where they share 448 tokens, while the whole tables
+//     are 256 MB of K and V: 64 x 8 heads of 128 17.2 -> 15.3, 256 x 8 of 64 28.2 -> 27.4; at the limit 128 x 8
+//     of 128 21.0 -> 24.5 but 30.2 -> 25.4 at 256 x 8, 256 tokens; not 512 x 8 of 64: 36 -> 50, 1024 x 8 of 128: 66 -> 160
+//   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 21.4 -> 16.5, 32 x 8 24.7 -> 18.3 (10 x 55
+//     32.9 -> 33.8); not 8 x 8: 15.1 -> 16.3, 1 x 8: 11.7 -> 14.2; shared, from 128 to 256
+//     groups: 32 x 8 21.2 -> 16.2, 24 x 8 20.2 -> 15.6; not 64 x 8: 25.0 -> 25.4, 128 x 8: 34.0 -> 43.1
+//   up to 2048, nothing shared, where G >= 512 fills its turns of 512 groups within 1.3 times: 250 x 8 117
+//     -> 100, 200 x 8 181 -> 152, 24 x 55 114 -> 101; past 1.3 either may win: 20 x 55 92 -> 83, 131 x 8 105
+//     -> 118; 10 x 55, 1.86: 59 -> 65
+// Longer ones would leave one long sequence among short ones to one group.
+constexpr int kWholeKeys = 512, kWholeMore = 1024, kWholeMost = 2048, kWholeGroups = 128, kWholeShared = 256;
+constexpr int64_t kWholeBytes = 256 << 20;
+
+bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles, int key_bytes) {
+  const int64_t keys = (int64_t)c.max_pages * c.page, groups = a.batch * tiles * c.kv_heads;
+  if (keys <= kWholeKeys) return !shared || groups * keys * key_bytes <= kWholeBytes;
+  if (keys > (shared ? kWholeMore : kWholeMost)) return false;
+  if (keys <= kWholeMore) return groups >= kWholeGroups && (!shared || groups <= kWholeShared);
+  return groups >= kHold && (groups + kHold - 1) / kHold * kHold * 10 <= groups * 13;
+}
+
 // ---------------------------------------------------------------------------
 // A piece of up to 16 NT rows.  Its keys go through registers only: a wave
 // takes every fourth tile of 32 keys, loads K rows as the A operand of
@@ -522,7 +546,7 @@ size_t prefix_workspace_bytes(const Cache& c, const Queries& a) { return space_b
 hipError_t launch_prefix(const Cache& c, const Queries& a, const void* q, const void* kp, const void* vp, const int32_t* tables,
                          const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse, void* ws,
                          hipStream_t st) {
-  const Args x = make_args(c, a, 4 * c.head_dim, q, kp, vp, tables, lens, ids, shared, o, lse, ws);
+  const Args x = make_args(c, a, 4 * c.head_dim, never_cut, q, kp, vp, tables, lens, ids, shared, o, lse, ws);
   switch (c.head_dim + x.tile) {
     case 64 + 16: return launch<64, 1>(x, st);
     case 96 + 16: return launch<96, 1>(x, st);

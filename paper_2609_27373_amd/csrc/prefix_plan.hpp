@@ -56,35 +56,12 @@ constexpr int kPreTile = 32, kWideRows = 64;
 // which a wave takes them alone, four heads a group, since the latency of a piece is most of
 // its time (128 sequences of up to 64 tokens over a 16K prefix, 64 heads of 64 on 16: 92 us
 // instead of 103).
-constexpr int kNarrowKeys = 128, kHold = 512;
+constexpr int kNarrowKeys = 128, kNarrowTable = 512, kHold = 512;   // kNarrowTable: of uncut ones, those of tables of so many
 
 constexpr int kSeeAll = 0x7fffffff - kMaxQueryRows;   // Piece::see of shared pages
 
 // Who plans: nobody (every sequence is one piece), every work-group, a launch before.
 enum { kWhole, kOwnPlan, kPlanned };
-// Whether every sequence is one piece, shared pages or not, which saves the plan and the
-// join.  By the tokens of a table (what a sequence can hold) and the groups G that this gives:
-//   up to 512: always, nothing shared.  1 x 301 tokens, 8 heads of 64: 12 -> 7.5 us; 1024 sequences of
-//     512 tokens, 8 heads of 128: 194 -> 161.  Where they share 448 tokens, while the whole tables
-//     are 256 MB of K and V: 64 x 8 heads of 128 17.2 -> 15.3, 256 x 8 of 64 28.2 -> 27.4; at the limit 128 x 8
-//     of 128 21.0 -> 24.5 but 30.2 -> 25.4 at 256 x 8, 256 tokens; not 512 x 8 of 64: 36 -> 50, 1024 x 8 of 128: 66 -> 160
-//   up to 1024, nothing shared, from 128 groups: 16 x 8 heads 21.4 -> 16.5, 32 x 8 24.7 -> 18.3 (10 x 55
-//     32.9 -> 33.8); not 8 x 8: 15.1 -> 16.3, 1 x 8: 11.7 -> 14.2; shared, from 128 to 256
-//     groups: 32 x 8 21.2 -> 16.2, 24 x 8 20.2 -> 15.6; not 64 x 8: 25.0 -> 25.4, 128 x 8: 34.0 -> 43.1
-//   up to 2048, nothing shared, where G >= 512 fills its turns of 512 groups within 1.3 times: 250 x 8 117
-//     -> 100, 200 x 8 181 -> 152, 24 x 55 114 -> 101; past 1.3 either may win: 20 x 55 92 -> 83, 131 x 8 105
-//     -> 118; 10 x 55, 1.86: 59 -> 65
-// Longer ones would leave one long sequence among short ones to one group.
-constexpr int kWholeKeys = 512, kWholeMore = 1024, kWholeMost = 2048, kWholeGroups = 128, kWholeShared = 256;
-constexpr int64_t kWholeBytes = 256 << 20;
-
-bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles, int key_bytes) {
-  const int64_t keys = (int64_t)c.max_pages * c.page, groups = a.batch * tiles * c.kv_heads;
-  if (keys <= kWholeKeys) return !shared || groups * keys * key_bytes <= kWholeBytes;
-  if (keys > (shared ? kWholeMore : kWholeMost)) return false;
-  if (keys <= kWholeMore) return groups >= kWholeGroups && (!shared || groups <= kWholeShared);
-  return groups >= kHold && (groups + kHold - 1) / kHold * kHold * 10 <= groups * 13;
-}
 
 struct Space {                         // the workspace
   int32_t* count;
@@ -808,8 +785,9 @@ join_kernel(Args x, int64_t all) {
   if (lane == 0 && x.lse != nullptr) x.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l)) * kLn2;
 }
 
-// The arguments of the kernels of one call.
-inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const void* q, const void* kp, const void* vp, const int32_t* tables,
+// The arguments of the kernels of one call.  whole: whether every sequence is one piece (never_cut).
+inline Args make_args(const Cache& c, const Queries& a, int key_bytes, bool (*whole)(const Cache&, const Queries&, bool, int64_t, int),
+                      const void* q, const void* kp, const void* vp, const int32_t* tables,
                       const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse, void* ws) {
   Space s;
   space_bytes(c, a, ws, &s);
@@ -821,12 +799,12 @@ inline Args make_args(const Cache& c, const Queries& a, int key_bytes, const voi
   x.rows = a.heads / c.kv_heads * a.q_len;
   x.tiles = (x.rows + x.tile - 1) / x.tile;
   x.key_bytes = key_bytes;
-  x.mode = never_cut(c, a, shared != nullptr, x.tiles, x.key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
+  x.mode = whole(c, a, shared != nullptr, x.tiles, key_bytes) ? kWhole : a.batch <= 256 ? kOwnPlan : kPlanned;
   if (x.mode == kWhole) shared = nullptr;
   x.wide_cost = x.shares = 0;
   x.mid_keys = kMidKeys, x.fill_all = 0, x.wide_keys = kWideKeys;
   x.page_bits = __builtin_ctz(c.page);
-  x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kWholeKeys);
+  x.narrow = (int64_t)a.batch * c.kv_heads > kHold && (x.mode != kWhole || c.max_pages * c.page <= kNarrowTable);
   x.most = x.mode == kWhole ? a.batch * x.tiles : (int)limits(c, a).pieces;
   x.q = (const uint16_t*)q, x.kp = (const uint16_t*)kp, x.vp = (const uint16_t*)vp;
   x.tables = tables, x.lens = lens, x.ids = ids, x.shared = shared;

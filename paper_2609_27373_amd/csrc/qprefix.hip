@@ -16,6 +16,23 @@
 namespace wise {
 namespace {
 
+// Whether every sequence is one piece, which saves the plan and the join, 7 to 10 us, and reads shared pages once for each.
+// By the tokens of a table (what a sequence can hold) and the groups G that this gives, us a call cut and whole,
+// 8 heads of 128 in 4 bits:
+//   nothing shared: up to 2048 always.  1 x 640 12.8 and 8.7, 32 x 1536 23.5 and 15.4, 48 x 2048 27.5 and 22.1, 1 x 2048 15.5
+//     and 16.0; up to 2560 with G of 192 to 1024, which fill the chip without ending one by one
+//   shared: up to 2048 while whole tables are at most 2^20 keys of a head, and 144 MB: 64 over 576 21.0 and 11.3, 32 over 1984
+//     22.2 and 16.6, 64 over 1984 24.1 and 22.0; not 128 over 1472, 28.0 and 32.4, nor 256 over 960, 36 and 47, nor 76 over 576 with
+//     15 heads in 8 bits, 183 MB, 24.5 and 28.9
+constexpr int kWholeMore = 2048, kWholeMost = 2560, kWholeFew = 192, kWholeMany = 1024;
+constexpr int64_t kWholeShared = 1 << 20, kWholeBytes = 144 << 20;
+
+bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles, int key_bytes) {
+  const int64_t keys = (int64_t)c.max_pages * c.page, groups = a.batch * tiles * c.kv_heads;
+  if (shared) return keys <= kWholeMore && groups * keys <= kWholeShared && groups * keys * key_bytes <= kWholeBytes;
+  return keys <= kWholeMore || (keys <= kWholeMost && groups >= kWholeFew && groups <= kWholeMany);
+}
+
 // ---------------------------------------------------------------------------
 // A piece of up to R rows (8, 16, 32).  A wave takes every fourth tile of 32 keys (S^T = K Q^T and
 // O^T = V^T P^T in 16x16x32 MFMAs, queries in columns).  The sums may run in
@@ -607,7 +624,7 @@ size_t qprefix_workspace_bytes(const Cache& c, const Queries& a) { return space_
 hipError_t launch_qprefix(const Cache& c, int bits, const Queries& a, const void* q, const void* kp, const void* vp,
                           const int32_t* tables, const int32_t* lens, const int32_t* ids, const int32_t* shared, void* o, float* lse,
                           void* ws, hipStream_t st) {
-  Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), q, kp, vp, tables, lens, ids, shared, o, lse, ws);
+  Args x = make_args(c, a, kept_key_bytes(c.head_dim, bits), never_cut, q, kp, vp, tables, lens, ids, shared, o, lse, ws);
   // Pieces are shorter work than in bf16, those of many rows the least so: a key to 128 rows takes three times one to few (128
   // over a 32K document 170 us dealt as equal, 159 as once, 145 as twice or more often), pieces of few rows may be longer, those of
   // many shorter (document 143 -> 137, 16 x 5 drafts 26.2 -> 25.7).

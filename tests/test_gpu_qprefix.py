@@ -64,9 +64,9 @@ class Batch:
         self.k, self.v = read_pool(pool, page, d, bits)
 
     def roomy(self):
-        """The same cache with tables of more than 2048 tokens, which are cut and joined however few sequences hold."""
+        """The same cache with tables of more than 2560 tokens, which are cut and joined however few sequences hold."""
         c = self.cache.shape
-        cols = max(c.max_pages, 2048 // c.page + 2)
+        cols = max(c.max_pages, 2560 // c.page + 2)
         tables = torch.full((c.seqs, cols), -1, dtype=torch.int32, device="cuda")
         tables[:, :c.max_pages] = self.cache.tables
         return QuantCache(1, c.pages, c.page, c.kv_heads, c.head_dim, c.seqs, cols, bits=self.bits, pool=self.cache.pool, tables=tables,
