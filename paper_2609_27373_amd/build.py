@@ -2,7 +2,7 @@
 
     python -m paper_2609_27373_amd.build
 
-Every HIP source under csrc/ is compiled into one shared library next to this
+Every HIP source under csrc/ is compiled, eight at a time, into one shared library next to this
 file.  The packed-fp32 feature is disabled for device code; hipcc's host pass
 prints a harmless warning that it does not know the feature.
 """
@@ -25,7 +25,7 @@ def sources():
 
 
 def command(out=LIB):
-    return (["/opt/rocm/bin/hipcc", f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-shared",
+    return (["/opt/rocm/bin/hipcc", "-parallel-jobs=8", f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-shared",
              "-fPIC", "-Wall", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")]
             + sources() + ["-o", out])
