@@ -44,8 +44,8 @@ bool never_cut(const Cache& c, const Queries& a, bool shared, int64_t tiles, int
 //      (D / 16) n .., widens a pair of dims of all eight keys, and two permutes a register make the A
 //      operands of two MFMAs, row m of the t-th being dim (D / 16) m + t
 // Of up to 8 rows the 16 columns hold each twice, and the second half of the columns does the softmax of the second 16
-// keys: half the exponentials (1%).  kTilesAhead tiles are in flight in registers; a third one, or more waves than
-// two a SIMD, did no better (one of 128K tokens: 44 us with two, 45 with three, 46 with four).
+// keys: half the exponentials (1%).  kTilesAhead tiles are in flight in registers; more did no
+// better (one of 128K tokens: 44 us with two, 45 with three, 46 with four), nor did three waves a SIMD instead of two (45).
 // Bound by HBM while tiles run, 1.05 us a tile of 32 keys of 128 in 4 bits with 2048 waves at work (8.5 TB/s, part of it from
 // the last-level cache).  A call has 10 to 15 us beside that: launch, plan (2 to 4), a piece's page ids and first
 // tiles (3.5), its join (1), the join of pieces (5).
