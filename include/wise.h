@@ -683,7 +683,8 @@ wise_status wise_qcache_compact(const wise_cache* c, int32_t bits,
  * those that were kept, as exact as they are there.  A NaN value makes its dim NaN in every row that
  * sees it, whatever its weight, and in no other; a NaN key the whole row.
  * Probabilities enter the product with V with 11 bits (where scales of values are outside 2^-23..2^8,
- * for 8 bits 2^-15..2^7, with 16).  Sums take up to 14 binades of fp32's range: values of 2^112 and
+ * for 8 bits 2^-15..2^7, or scores, times scale log2(e), past 2^20, with 16).  Finite scores give finite
+ * weights, whatever their size.  Sums take up to 14 binades of fp32's range: values of 2^112 and
  * more may give infinities.
  *
  *   workspace : wise_qcache_workspace_bytes(c, bits, a) bytes, 256-byte aligned.

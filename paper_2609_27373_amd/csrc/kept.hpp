@@ -69,6 +69,11 @@ __device__ __forceinline__ uint32_t past_half(uint32_t w) {
   return B == 4 ? ((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u : ~((w + 0x10101010u) & (w + 0x79797979u)) & 0x80808080u;
 }
 
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {   // of two 16-bit numbers each
+  typedef uint16_t U2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(U2, a), __builtin_bit_cast(U2, b)));
+}
+
 // Scale byte i of a word, as widen_pair takes it.
 __device__ __forceinline__ float scale_of(uint32_t w, int i) {
   return __builtin_bit_cast(float, i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1);

@@ -15,11 +15,7 @@
 namespace wise {
 namespace {
 
-__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {   // of two 16-bit numbers each
-  typedef uint16_t U2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(U2, a), __builtin_bit_cast(U2, b)));
-}
-__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {   // of two 16-bit numbers each
   typedef uint16_t U2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(U2, a), __builtin_bit_cast(U2, b)));
 }

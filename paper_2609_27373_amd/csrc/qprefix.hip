@@ -8,8 +8,9 @@
 // the matrix cores take it, and a score is as exact as with keys in bf16.  Values are widened to fp16 where that
 // is exact too, which their scales tell (past_half), and meet probabilities of 11 bits in one MFMA: o is off by
 // 2^-12 of sum p |v| at most beside its own rounding of 2^-8, and measures 0.16 to 0.17% rms from its definition as
-// with exact probabilities.  Else both are bf16 and a probability is two numbers (split_bf16x2), an MFMA more.  One
-// number instead of two everywhere took 32 x 8K tokens from 45 to 44 us, 128 over a 32K document from 203 to 171.
+// with exact probabilities.  Else, and where a row's reference is past kHalfReach, both are bf16 and a probability is two numbers
+// (split_bf16x2), an MFMA more.  One number instead of two everywhere took 32 x 8K tokens from 45 to 44 us, 128 over a 32K document from 203
+// to 171.
 #include "kept.hpp"
 #include "prefix_plan.hpp"
 
@@ -82,12 +83,30 @@ __device__ __forceinline__ void put_nan(const Args& x, const int32_t* table, int
   }
 }
 
+// What a row's exponents are taken against when its largest score becomes mx: kHalfLow below it, or, from 2^24 on, where fp32's
+// steps are too large for that, the number at or next below it: mx has then a probability from 1 up to 2^(a step).  From 2^30 on that
+// may be infinite, and is taken as kFarMost: what is less than a step apart there has equal weights.
+constexpr float kFarMost = 0x1p64f;
+__device__ __forceinline__ float reference(float mx, float sc) {
+  const float s = mx * sc;
+  if (__builtin_fabsf(s) < 0x1p24f) return s - kHalfLow;
+  const int bits = __builtin_bit_cast(int, s);
+  return __builtin_fmaf(mx, sc, -s) < 0.f ? __builtin_bit_cast(float, s > 0.f ? bits - 1 : bits + 1) : s;
+}
+
 // threadIdx.x, unknown to the compiler, which would else keep what a piece computes from it
 // over the loop over pieces.
 __device__ __forceinline__ int fresh_tid() {
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
   return tid;
+}
+
+// A constant in a scalar register, unknown to the compiler, which would else keep it in vector registers over the loop over
+// pieces (infinities among 16 of them, spilled and read back for each tile with a mask).
+__device__ __forceinline__ float scalar(float c) {
+  asm volatile("" : "+s"(c));
+  return c;
 }
 
 // The kernel's argument where the hardware has put it, unknown to the compiler, which would else keep what it has read of it,
@@ -128,7 +147,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   float m[NT], l[NT];
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
-    m[u] = -INFINITY;
+    m[u] = scalar(-INFINITY);
     l[u] = 0.f;
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[u][t] = f32x4_t{};
@@ -210,12 +229,13 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
       for (int r = 0; r < kS; ++r) y[u][r] = kPack ? (n < 8 ? s[u][0][r] : s[u][1][r]) : s[u][r >> 2][r & 3];
     if (masked) {
+      const float none = scalar(-INFINITY);
 #pragma unroll
       for (int u = 0; u < NT; ++u)
 #pragma unroll
         for (int r = 0; r < kS; ++r) {
           const bool second = kPack ? n >= 8 : r >= 4;
-          if (key0 + (second ? 16 : 0) + 4 * g + (r & 3) >= see[u] || !(second ? ok1 : ok0)) y[u][r] = -INFINITY;
+          if (key0 + (second ? 16 : 0) + 4 * g + (r & 3) >= see[u] || !(second ? ok1 : ok0)) y[u][r] = none;
         }
       // Values that no row sees may be anything, and NaN must not reach the rows that don't see
       // it (0 * NaN is NaN): they count as 0 or as some number, and the rows that see NaN get it at the end.
@@ -244,7 +264,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < (D == 96 ? 2 : 1); ++j) far |= past_half<B>(w.vs[h][j]);
-    const bool half = __builtin_amdgcn_ballot_w64(far != 0) == 0;
+    bool half = __builtin_amdgcn_ballot_w64(far != 0) == 0, past = false;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       float mx = y[u][0];
@@ -253,9 +273,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       // The reference of the exponents is raised as kProbHalf says, not for each new maximum.
       if (__builtin_amdgcn_ballot_w64(mx * x.sc > m[u] + kHalfTop)) {
         if constexpr (kPack) mx = fmaxf(mx, dpp_mov<0x128>(mx));   // row_ror 8
-        mx = quad_max(mx) * x.sc;
-        const bool grow = mx > m[u] + kHalfTop;
-        const float mn = grow ? mx - kHalfLow : m[u];
+        mx = quad_max(mx);
+        const bool grow = mx * x.sc > m[u] + kHalfTop;
+        const float mn = grow ? reference(mx, x.sc) : m[u];
         const float alpha = grow ? fast_exp2(m[u] - mn) : 1.f;
         l[u] *= alpha;
 #pragma unroll
@@ -265,12 +285,23 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
         m[u] = mn;
       }
       const float mb = m[u] == -INFINITY ? 0.f : m[u];
+      past |= __builtin_fabsf(mb) >= kHalfReach;
+#pragma unroll
+      for (int r = 0; r < kS; ++r) y[u][r] = fast_exp2(__builtin_fmaf(y[u][r], x.sc, -mb));
+    }
+    if (__builtin_amdgcn_ballot_w64(past)) {
+      half = false;
+      const float most = scalar(kFarMost);
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int r = 0; r < kS; ++r) y[u][r] = y[u][r] > most ? most : y[u][r];
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
       float ts = 0.f;
 #pragma unroll
-      for (int r = 0; r < kS; ++r) {
-        y[u][r] = fast_exp2(__builtin_fmaf(y[u][r], x.sc, -mb));
-        ts += y[u][r];
-      }
+      for (int r = 0; r < kS; ++r) ts += y[u][r];
       l[u] += ts;
     }
     // Values in fp16 and probabilities with 11 bits where that is exact for the values, else both in bf16 and the
@@ -328,7 +359,10 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   }
   // Join the waves.
   float* mls = lds + 4 * kRows * kStride;
-  const bool poisoned = __syncthreads_or(poison != 0);
+  int32_t* flags = (int32_t*)(mls + 8 * kRows);     // per wave: it has set NaN values aside
+  __syncthreads();
+  const int mine = __builtin_amdgcn_ballot_w64(poison != 0) != 0;
+  if (lane == 0) flags[wave] = mine;
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     float lt = quad_sum(l[u]);
@@ -344,14 +378,16 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       for (int t = 0; t < kT; t += 2) *(f32x2_t*)(lds + r * kStride + kT * (4 * g + i) + t) = f32x2_t{o[u][t][i], o[u][t + 1][i]};
   }
   __syncthreads();
+  const bool poisoned = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
   if (my_head >= x.c.kv_heads) return;
   for (int j = kAlone ? lane : tid; j < p.rows * (D / 4); j += kAlone ? 64 : 256) {
     const int r = j / (D / 4), d = j % (D / 4) * 4;
-    float mw[4], mx = -INFINITY, lt = 0.f;
+    const float none = scalar(-INFINITY);
+    float mw[4], mx = none, lt = 0.f;
     f32x4_t sum{};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      mw[w] = kAlone && w != wave ? -INFINITY : mls[2 * (w * kRows + r)];
+      mw[w] = kAlone && w != wave ? none : mls[2 * (w * kRows + r)];
       mx = fmaxf(mx, mw[w]);
     }
     const float mb = mx == -INFINITY ? 0.f : mx;
@@ -376,24 +412,77 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   }
 }
 
+// This lane's half of its row of Q in a piece of many rows.
+template <int D>
+__device__ __forceinline__ const uint16_t* tile_query(const Args& x, const Piece& p, int wave, int lane) {
+  const int r = p.row0 + min(32 * wave + (lane & 31), p.rows - 1);
+  const int b = p.first + r / x.rows;
+  return x.q + (((size_t)b * x.c.kv_heads + p.head) * x.rows + r % x.rows) * D + 8 * (lane >> 5);
+}
+
+// Whether tile_piece can do a piece: all page ids name pages, fp16 holds its values by their scales, and no score
+// is past kHalfReach by the largest scale of its keys and the largest number of Q.  A thread looks at four tokens at a time.
+// Beside tile_piece, not in it, where the compiler kept what the two share in registers over the loop.  most: 4 words of LDS
+// that tile_piece leaves alone.
+template <int D, int B>
+__device__ __forceinline__ bool tile_ready(const Args& x, const Piece& p, int32_t* most) {
+  using L = Kept<D, B>;
+  const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int page = x.c.page;
+  const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
+  const uint16_t* row = tile_query<D>(x, p, wave, lane);
+  u32x4_t q[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) q[i] = *(const u32x4_t*)(row + 16 * i);
+  uint32_t bad = 0, k_most = 0, q_most = 0;         // q_most: bits of two numbers without their signs
+  for (int t = p.k0 + 4 * tid; t < p.k1; t += 1024) {
+    const int id = table[t >> x.page_bits], at = t & (page - 1);
+    if (!in_range(id, x.c.pages)) {
+      bad = 1;
+      break;
+    }
+    const size_t scales = ((size_t)id * x.c.kv_heads + p.head) * (page * (L::kRow + L::kScales)) + page * L::kRow;
+    const char *ks = (const char*)x.kp + scales + at * L::kScales, *vs = (const char*)x.vp + scales;
+#pragma unroll
+    for (int i = 0; i < L::kScales; ++i) {
+      bad |= past_half<B>(*(const uint32_t*)(vs + L::v_scale(at, i)));
+      const uint32_t k = *(const uint32_t*)(ks + 4 * i);
+      k_most = max_pair(k_most, max_pair(k & 0xff00ff, k >> 8 & 0xff00ff));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q_most = max_pair(q_most, q[i][j] & 0x7fff7fff);
+  const auto larger = [](int x, int y) { return (int)max_pair((uint32_t)x, (uint32_t)y); };
+  const int w = wave_scan((int)(max(q_most & 0xffff, q_most >> 16) | max(k_most & 0xffff, k_most >> 16) << 16), 0, larger);
+  if (lane == 63) most[wave] = w;
+  const int refused = __syncthreads_or(bad != 0);
+  const uint32_t all = max_pair(max_pair(most[0], most[1]), max_pair(most[2], most[3]));
+  const float top = x.sc * (D * (B == 4 ? 6.f : 448.f)) * __builtin_bit_cast(float, all << 16) * scale_of(all >> 16, 0);
+  return __builtin_amdgcn_readfirstlane(!refused && top < kHalfReach);   // the same in every lane
+}
+
 // ---------------------------------------------------------------------------
 // A piece of up to 128 rows, all of which see all its keys (whole tiles of 64): the
 // pipeline of the dense kernel (WaveRows::step), four waves of 32 rows over rings of two K
 // and two V tiles in LDS, in bf16: a wave widens 16 consecutive keys of a tile, which lie in one page, for
 // all four, a tile ahead of their use, from registers that were loaded a step before.  Bound by the exponentials and the
 // latency of two waves a SIMD: 1.5 us a tile of 64 keys of 128 alone on a CU, 2.1 beside a group of few rows (512 rows over
-// 32K tokens 108 us, 147 when 32 rows at a time were streamed).  False, with nothing done, if some page id of the piece names
-// no page, or a scale of its values is past what fp16 holds.
+// 32K tokens 108 us, 147 when 32 rows at a time were streamed).  Only where tile_ready
+// says so.
 // ---------------------------------------------------------------------------
 template <int D, int B>
-__device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* smem) {
+__device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, char* smem) {
   using L = Kept<D, B>;
   using G = Geo<D>;
   using S = Swizzle<D>;
   constexpr int kT = S::kTile, kC = D / 32, kWords = L::kWords;
   const int tid = fresh_tid(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, n = lane & 15;
-  const int rows = x.rows, page = x.c.page, kh = p.head;
+  const int page = x.c.page;
+  int kh = p.head;
+  asm volatile("" : "+s"(kh));                      // in a scalar register: addresses computed with it are then scalars too
   const int32_t* table = x.tables + (size_t)p.table * x.c.max_pages;
   const int tiles = (p.k1 - p.k0) / kKeyTile;
   // Page ids of this wave's keys: lane i has the one of tile 64 u + i, of stretch u and the next one.
@@ -402,25 +491,10 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
     return key < p.k1 ? table[key >> x.page_bits] : 0;
   };
   int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
-  // All pages there, and all scales of values such that fp16 holds the values: those of four tokens a thread.
-  uint32_t bad = 0;
-  for (int t = p.k0 + 4 * tid; t < p.k1; t += 1024) {
-    const int id = table[t >> x.page_bits];
-    if (!in_range(id, x.c.pages)) {
-      bad = 1;
-      break;
-    }
-    const char* scales = (const char*)x.vp + ((size_t)id * x.c.kv_heads + kh) * (page * (L::kRow + L::kScales)) + page * L::kRow;
-#pragma unroll
-    for (int i = 0; i < L::kScales; ++i) bad |= past_half<B>(*(const uint32_t*)(scales + L::v_scale(t & (page - 1), i)));
-  }
-  if (__syncthreads_or(bad != 0)) return false;
   WaveRows<D> w;
   w.reset();
   {
-    const int r = p.row0 + min(32 * wave + (lane & 31), p.rows - 1);
-    const int b = p.first + r / rows;
-    const uint16_t* row = x.q + (((size_t)b * x.c.kv_heads + kh) * rows + r % rows) * D + 8 * (lane >> 5);
+    const uint16_t* row = tile_query<D>(x, p, wave, lane);
 #pragma unroll
     for (int i = 0; i < G::kDChunks; ++i) w.qf[i] = *(const u32x4_t*)(row + 16 * i);
   }
@@ -537,11 +611,11 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
     s0[1] = s1[1];
     ++it;
   }
-  if (!active) return true;
+  if (!active) return;
   w.template step<2, false, true, 0, kProbHalf>(sk, sv + (it & 1) * kT, ra, lane, x.sc, s0, s1, mx, [](auto, int) {}, [](f32x16_t*) {});
   const float lt = pair_sum(w.l);
   const int q = 32 * wave + (lane & 31), h = lane >> 5;
-  if (q >= p.rows) return true;
+  if (q >= p.rows) return;
   const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + q;
 #pragma unroll
   for (int t = 0; t < G::kDTiles; ++t)
@@ -550,7 +624,6 @@ __device__ __forceinline__ bool tile_piece(const Args& x, const Piece& p, char* 
       *(f32x4_t*)(x.part + at * D + 32 * t + 8 * j + 4 * h) =
           f32x4_t{w.o[t][4 * j], w.o[t][4 * j + 1], w.o[t][4 * j + 2], w.o[t][4 * j + 3]};
   if (h == 0) x.ml[at] = float2{w.m, lt};
-  return true;
 }
 
 // Pieces of a group, at most: with 8 some calls had more groups than the chip holds at once, which planned in a second turn (64
@@ -560,7 +633,7 @@ constexpr int kMine = 16;
 template <int D, int B, int R, bool kShared>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 qpiece_kernel(Args x) {
-  constexpr int kJoin = 4 * 16 * (kShared || R == 32 ? 2 : 1) * (D + 6) * 4, kRing = kShared ? 4 * Swizzle<D>::kTile : 0;
+  constexpr int kJoin = 4 * 16 * (kShared || R == 32 ? 2 : 1) * (D + 6) * 4 + 16, kRing = kShared ? 4 * Swizzle<D>::kTile + 16 : 0;
   __shared__ __attribute__((aligned(1024))) char smem[kJoin > kRing ? kJoin : kRing];
   static_assert(sizeof(Plan<256>) <= sizeof(smem), "the plan fits");
   __shared__ Piece todo[kMine];
@@ -580,7 +653,10 @@ qpiece_kernel(Args x) {
       for (int j = 0; j < 11; ++j) w[j] = __builtin_amdgcn_readfirstlane(w[j]);
       if (p.rows == 0) continue;
       if (i > 0) __syncthreads();                   // the piece before has left the LDS
-      if (kShared && p.kind == kManyRows && tile_piece<D, B>(fresh_args(), p, smem)) continue;
+      if (kShared && p.kind == kManyRows && tile_ready<D, B>(fresh_args(), p, (int32_t*)(smem + 4 * Swizzle<D>::kTile))) {
+        tile_piece<D, B>(fresh_args(), p, smem);
+        continue;
+      }
       if (p.kind == kNarrow) {
         stream_piece<D, B, R, true>(fresh_args(), p, (float*)smem);
         continue;
