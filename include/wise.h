@@ -684,8 +684,8 @@ wise_status wise_qcache_compact(const wise_cache* c, int32_t bits,
  * sees it, whatever its weight, and in no other; a NaN key the whole row.
  * Probabilities enter the product with V with 11 bits (where scales of values are outside 2^-23..2^8,
  * for 8 bits 2^-15..2^7, or scores, times scale log2(e), past 2^20, with 16).  Finite scores give finite
- * weights, whatever their size.  Sums take up to 14 binades of fp32's range: values of 2^112 and
- * more may give infinities.
+ * weights, whatever their size.  o is finite where the values of a dim that a row sees add up, by
+ * magnitude, to less than 2^127 (an average of larger ones may come out infinite or NaN).
  *
  *   workspace : wise_qcache_workspace_bytes(c, bits, a) bytes, 256-byte aligned.
  * The others, and the errors, as for wise_prefix_attn (WISE_ERR_UNSUPPORTED

@@ -83,13 +83,13 @@ __device__ __forceinline__ void put_nan(const Args& x, const int32_t* table, int
   }
 }
 
-// What a row's exponents are taken against when its largest score becomes mx: kHalfLow below it, or, from 2^24 on, where fp32's
+// What a row's exponents are taken against when its largest score becomes mx: `low` below it, or, from 2^24 on, where fp32's
 // steps are too large for that, the number at or next below it: mx has then a probability from 1 up to 2^(a step).  From 2^30 on that
 // may be infinite, and is taken as kFarMost: what is less than a step apart there has equal weights.
 constexpr float kFarMost = 0x1p64f;
-__device__ __forceinline__ float reference(float mx, float sc) {
+__device__ __forceinline__ float reference(float mx, float sc, float low) {
   const float s = mx * sc;
-  if (__builtin_fabsf(s) < 0x1p24f) return s - kHalfLow;
+  if (__builtin_fabsf(s) < 0x1p24f) return s - low;
   const int bits = __builtin_bit_cast(int, s);
   return __builtin_fmaf(mx, sc, -s) < 0.f ? __builtin_bit_cast(float, s > 0.f ? bits - 1 : bits + 1) : s;
 }
@@ -103,7 +103,7 @@ __device__ __forceinline__ int fresh_tid() {
 }
 
 // A constant in a scalar register, unknown to the compiler, which would else keep it in vector registers over the loop over
-// pieces (infinities among 16 of them, spilled and read back for each tile with a mask).
+// pieces (infinities among 16 of them, spilled, and read back for each tile with a mask).
 __device__ __forceinline__ float scalar(float c) {
   asm volatile("" : "+s"(c));
   return c;
@@ -177,7 +177,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       // Of the page's scales, those of token t are (kRow - kScales) t bytes nearer than its codes.
       w.apart[s] = page * L::kRow - ((begin + stride * i + 16 * s) & (page - 1)) * (L::kRow - L::kScales);
       const char* codes = kp + w.at[s];
-      load_words<kWords, B == 4>(codes + k_code, w.k[s]);
+      uint32_t at = k_code;                           // NT = 2: its 64 bits anew, which the compiler would else spill
+      if constexpr (NT == 2) asm volatile("" : "+v"(at));
+      load_words<kWords, B == 4>(codes + at, w.k[s]);
       w.ks[s][0] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_scale));
       if constexpr (D == 96) w.ks[s][1] = *(const uint8_t*)(codes + (uint32_t)(w.apart[s] + k_last));
     }
@@ -186,7 +188,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const char* codes = vp + w.at[s];
-      load_words<kWords>(codes + v_code, w.v[s]);
+      uint32_t at = v_code;
+      if constexpr (NT == 2) asm volatile("" : "+v"(at));
+      load_words<kWords>(codes + at, w.v[s]);
       w.vs[s][0] = *(const uint32_t*)(codes + (uint32_t)(w.apart[s] + v_scale));
       if constexpr (D == 96) w.vs[s][1] = *(const uint32_t*)(codes + (uint32_t)(w.apart[s] + v_last));
     }
@@ -270,12 +274,14 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       float mx = y[u][0];
 #pragma unroll
       for (int r = 1; r < kS; ++r) mx = fmaxf(mx, y[u][r]);
-      // The reference of the exponents is raised as kProbHalf says, not for each new maximum.
-      if (__builtin_amdgcn_ballot_w64(mx * x.sc > m[u] + kHalfTop)) {
+      // The reference of the exponents is raised as kProbHalf says, not for each new maximum; where values are not in fp16 for
+      // each, since a weight above 1 could take their sum out of fp32's range.
+      if (!half || __builtin_amdgcn_ballot_w64(mx * x.sc > m[u] + kHalfTop)) {
+        const float top = half ? kHalfTop : 0.f, low = half ? kHalfLow : 0.f;
         if constexpr (kPack) mx = fmaxf(mx, dpp_mov<0x128>(mx));   // row_ror 8
         mx = quad_max(mx);
-        const bool grow = mx * x.sc > m[u] + kHalfTop;
-        const float mn = grow ? reference(mx, x.sc) : m[u];
+        const bool grow = mx * x.sc > m[u] + top;
+        const float mn = grow ? reference(mx, x.sc, low) : m[u];
         const float alpha = grow ? fast_exp2(m[u] - mn) : 1.f;
         l[u] *= alpha;
 #pragma unroll
@@ -407,7 +413,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       const size_t at = ((size_t)p.first * x.c.kv_heads + kh) * rows + p.row0 + r;
       const float inv = lt == 0.f ? 0.f : 1.f / lt;
       *(u32x2_t*)(x.o + at * D + d) = u32x2_t{pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv)};
-      if (d == 0 && x.lse != nullptr) x.lse[at] = lt == 0.f ? -INFINITY : (mx + __builtin_log2f(lt)) * kLn2;
+      if (d == 0 && x.lse != nullptr) x.lse[at] = lt == 0.f ? none : (mx + __builtin_log2f(lt)) * kLn2;
     }
   }
 }
@@ -493,6 +499,7 @@ __device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, char* 
   int stretch = 0, ids = load_ids(0), next_ids = load_ids(1);
   WaveRows<D> w;
   w.reset();
+  w.m = scalar(-INFINITY);
   {
     const uint16_t* row = tile_query<D>(x, p, wave, lane);
 #pragma unroll

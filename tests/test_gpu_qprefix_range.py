@@ -1,5 +1,5 @@
 """wise_qcache_attn on the GPU where numbers are very large: scores past 2^16 and up to fp32's largest, against the
-fp64 definition over scores that fp32 holds exactly."""
+fp64 definition over scores that fp32 holds exactly, and values whose sums reach the end of its range."""
 
 import numpy as np
 import pytest
@@ -67,4 +67,36 @@ def test_large_scores(gpu_lib, kind, d, sign, bits):
                 out, lse = b.run(shared, scale, cache=cache)
                 say(f"2^{power} d {d} bits {bits} {kind} shared {shared}")
                 assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+                b.check(out, lse, truth)
+
+
+@WIDTHS
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("gain", [0.0, 1.0, 8.0, 60.0])
+def test_large_values(gpu_lib, kind, d, gain, bits):
+    """Values that add up to just under 2^127 in a row's dims, in every scale or in one of them: o is finite."""
+    groups, kv, gq, q_len = KINDS[kind]
+    b = Batch(groups, 16, d, kv, gq, bits, q_len, seed=d, gain=gain)
+    n = int(b.lens.max())
+    largest = 127 + int(np.floor(127 - np.log2(n * (6 if bits == 4 else 448))))
+    pool = b.pool.copy()
+    at = 16 * d * bits // 8
+    scales = pool[1][..., at:]
+    live = scales != 255
+    of = np.zeros(scales.shape[-1], int)              # which 32 dims a scale is of
+    of[:] = np.arange(of.size) % (4 * d // 32) // 4
+    for which in (None, 0, d // 32 - 1):
+        new = scales.copy()
+        new[live & (of == which if which is not None else True)] = largest
+        pool[1][..., at:] = new
+        b.set_pool(pool, 16, d, bits)
+        b.cache.pool.copy_(torch.tensor(pool))
+        truth = b.truth()
+        assert np.abs(truth[0]).max() > 2.0 ** 100
+        for cache in (b.cache, b.roomy()):
+            for shared in (True, False):
+                out, lse = b.run(shared, cache=cache)
+                say(f"scale {which} d {d} bits {bits} {kind} gain {gain} shared {shared}")
+                assert torch.isfinite(out).all()
                 b.check(out, lse, truth)
