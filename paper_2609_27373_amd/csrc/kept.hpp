@@ -79,6 +79,9 @@ __device__ __forceinline__ float scale_of(uint32_t w, int i) {
   return __builtin_bit_cast(float, i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1);
 }
 
+// A word whose first n bytes are 255 (none for n < 0, all for n > 4).
+__device__ __forceinline__ uint32_t low_bytes(int n) { return n <= 0 ? 0u : ~0u >> (32 - 8 * min(n, 4)); }
+
 // The bytes of w that are 255, and (kCode) those whose lower seven bits are set, as 255.
 template <bool kCode>
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {

@@ -245,8 +245,8 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       // it (0 * NaN is NaN): they count as 0 or as some number, and the rows that see NaN get it at the end.
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int left = min(max(p.k1 - (key0 + 16 * h + 4 * g), 0), 4);
-        const uint32_t keep = !(h ? ok1 : ok0) || left == 0 ? 0u : ~0u >> (32 - 8 * left);
+        const int left = (h ? ok1 : ok0) ? min(max(p.k1 - (key0 + 16 * h + 4 * g), 0), 4) : 0;
+        const uint32_t keep = low_bytes(left);
 #pragma unroll
         for (int j = 0; j < (D == 96 ? 2 : 1); ++j) {
           const uint32_t bad = nan_bytes<false>(w.vs[h][j] & keep);
@@ -257,7 +257,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
 #pragma unroll
           for (int j = 0; j < kWords; ++j) {
             const uint32_t bad = nan_bytes<true>(w.v[h][j]);
-            poison |= bad;
+            poison |= bad & low_bytes(left * (D / 16) - 4 * j);   // those of tokens behind the last one are nobody's
             w.v[h][j] &= ~bad;
           }
         }
