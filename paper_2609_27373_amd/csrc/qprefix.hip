@@ -203,7 +203,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       load_v(raw[i]);
     }
   }
-  uint32_t poison = 0;                              // NaN values set aside
+  int poisoned = 0x7fffffff;                        // first key of the first tile that had NaN values set aside
   auto tile = [&](int i, Raw<D, B>& w) {
     const int key0 = begin + stride * i;
     const bool ok0 = w.ok[0], ok1 = w.ok[1];
@@ -243,6 +243,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
         }
       // Values that no row sees may be anything, and NaN must not reach the rows that don't see
       // it (0 * NaN is NaN): they count as 0 or as some number, and the rows that see NaN get it at the end.
+      uint32_t poison = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int left = (h ? ok1 : ok0) ? min(max(p.k1 - (key0 + 16 * h + 4 * g), 0), 4) : 0;
@@ -262,6 +263,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
           }
         }
       }
+      if (__builtin_amdgcn_ballot_w64(poison != 0)) poisoned = min(poisoned, key0);
     }
     uint32_t far = 0;                                 // a scale is past what fp16 holds
 #pragma unroll
@@ -365,10 +367,9 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
   }
   // Join the waves.
   float* mls = lds + 4 * kRows * kStride;
-  int32_t* flags = (int32_t*)(mls + 8 * kRows);     // per wave: it has set NaN values aside
+  int32_t* first = (int32_t*)(mls + 8 * kRows);     // the waves' `poisoned`
   __syncthreads();
-  const int mine = __builtin_amdgcn_ballot_w64(poison != 0) != 0;
-  if (lane == 0) flags[wave] = mine;
+  if (lane == 0) first[wave] = poisoned;
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     float lt = quad_sum(l[u]);
@@ -384,7 +385,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       for (int t = 0; t < kT; t += 2) *(f32x2_t*)(lds + r * kStride + kT * (4 * g + i) + t) = f32x2_t{o[u][t][i], o[u][t + 1][i]};
   }
   __syncthreads();
-  const bool poisoned = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+  poisoned = __builtin_amdgcn_readfirstlane(min(min(first[0], first[1]), min(first[2], first[3])));
   if (my_head >= x.c.kv_heads) return;
   for (int j = kAlone ? lane : tid; j < p.rows * (D / 4); j += kAlone ? 64 : 256) {
     const int r = j / (D / 4), d = j % (D / 4) * 4;
@@ -404,7 +405,7 @@ __device__ __forceinline__ void stream_piece(const Args& x, const Piece& p, floa
       lt += f * mls[2 * (w * kRows + r) + 1];
       sum += f * *(const f32x4_t*)(lds + (w * kRows + r) * kStride + d);
     }
-    if (poisoned) put_nan<D, B>(x, table, kh, p.k0, min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1), d, sum);
+    if (poisoned < p.k1) put_nan<D, B>(x, table, kh, poisoned, min(p.see + (p.row0 + r) % rows % x.a.q_len, p.k1), d, sum);
     if (p.slot >= 0) {
       const size_t at = (size_t)p.slot + (size_t)kh * p.seg_rows + p.row0 + r;
       *(f32x4_t*)(x.part + at * D + d) = sum;

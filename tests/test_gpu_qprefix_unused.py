@@ -1,4 +1,5 @@
-"""wise_qcache_attn on the GPU: what lies in places that no row sees changes neither its results nor its time."""
+"""wise_qcache_attn on the GPU: what lies in places that no row sees changes neither its results nor its time, and NaN that rows do
+see costs little."""
 
 import numpy as np
 import pytest
@@ -74,3 +75,52 @@ def test_unused_bytes_cost_nothing(gpu_lib, d, bits):
         times.append(time_of(b.cache, q, None, ids))
     say(f"d {d} bits {bits}: {times} us")
     assert max(times[1:]) < 3 * times[0]
+
+
+@WIDTHS
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_a_nan_costs_little(gpu_lib, d, bits):
+    """A NaN in the newest token's value: at most three times the time of none, as above."""
+    b = Batch([(0, [2033] * 8)], 16, d, 8, 4, bits, 1, seed=d)
+    q, ids = b.q.cuda(), ints(b.ids)
+    b.cache.pool.copy_(torch.tensor(np.where(used(b, d)[:, :, None], b.pool, 0)))
+    times = [time_of(b.cache, q, None, ids)]
+    for s in b.ids:
+        b.cache.pool[1, int(b.tables[s, 2032 // 16]), :, 16 * d * bits // 8] = 255      # the first scale of the page's first token
+    times.append(time_of(b.cache, q, None, ids))
+    out, _ = b.run()
+    nan = torch.isnan(out)
+    assert nan[..., :32].all() and not nan[..., 32:].any()
+    say(f"d {d} bits {bits}: {times} us")
+    assert times[1] < 3 * times[0]
+
+
+@WIDTHS
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("lens", [[700, 130, 40], [700, 3000]])
+def test_nan_beside_missing_pages(gpu_lib, d, lens, bits):
+    """NaN values in tiles that have a mask in the middle of a sequence, as half of their keys have no page, and in later ones."""
+    page, q_len = 16, 3
+    b = Batch([(0, lens)], page, d, 2, 4, bits, q_len, seed=d)
+    missing = [(s, c) for s, n in enumerate(lens) for c in (1, 6, 30) if c * page < n - page]
+    for s, c in missing:
+        b.tables[s, c] = -1
+    b.cache.tables.copy_(ints(b.tables.tolist()))
+    o, lse, bound, zb = b.truth()
+    row, g = d * bits // 8, d // 32
+    for hit in ([(0, 0, 0, 0)], [(0, 7 * page + 3, 1, 1), (0, 20 * page, 0, 0)], [(0, 699, 1, g - 1), (1, 7 * page + 1, 0, 1)],
+                [(s, n - q_len + 1, 0, 1) for s, n in enumerate(lens)]):      # sequence, position, head, scale
+        pool, want = b.pool.copy(), o.copy()
+        for s, pos, h, i in hit:
+            p, t = b.tables[s, pos // page], pos % page
+            assert p >= 0
+            pool[1, p, h, page * row + t // 4 * 4 * g + 4 * i + t % 4] = 255
+            for r in range(q_len):
+                if pos <= lens[s] - q_len + r:
+                    want[s, 4 * h:4 * h + 4, r, 32 * i:32 * i + 32] = np.nan
+        b.cache.pool.copy_(torch.tensor(pool))
+        for cache in (b.cache, b.roomy()):
+            got = b.run(False, cache=cache)[0].double().cpu().numpy()
+            assert np.array_equal(np.isnan(got), np.isnan(want)), hit
+            ok = ~np.isnan(want)
+            assert np.all(np.abs(got - want)[ok] <= bound[ok])
