@@ -683,7 +683,7 @@ wise_status wise_qcache_compact(const wise_cache* c, int32_t bits,
  * those that were kept, as exact as they are there.  A NaN value makes its dim NaN in every row that
  * sees it, whatever its weight, and in no other; a NaN key the whole row.
  * Probabilities enter the product with V with 11 bits (where scales of values are outside 2^-23..2^8,
- * for 8 bits 2^-15..2^7, or scores, times scale log2(e), past 2^20, with 16).  Finite scores give finite
+ * for 8 bits 2^-15..2^7, or scores, times scale log2(e), past 2^22, with 16).  Finite scores give finite
  * weights, whatever their size.  o is finite where the values of a dim that a row sees add up, by
  * magnitude, to less than 2^127 (an average of larger ones may come out infinite or NaN).
  *

@@ -474,10 +474,11 @@ __device__ __forceinline__ bool tile_ready(const Args& x, const Piece& p, int32_
 // A piece of up to 128 rows, all of which see all its keys (whole tiles of 64): the
 // pipeline of the dense kernel (WaveRows::step), four waves of 32 rows over rings of two K
 // and two V tiles in LDS, in bf16: a wave widens 16 consecutive keys of a tile, which lie in one page, for
-// all four, a tile ahead of their use, from registers that were loaded a step before.  Bound by the exponentials and the
-// latency of two waves a SIMD: 1.5 us a tile of 64 keys of 128 alone on a CU, 2.1 beside a group of few rows (512 rows over
-// 32K tokens 108 us, 147 when 32 rows at a time were streamed).  Only where tile_ready
-// says so.
+// all four, a tile ahead of their use, from registers that were loaded a step before.  Only where tile_ready says so.  Bound
+// by the latency of two waves a SIMD and by VALU work: of some 600 instructions of two tiles of 64 keys of 128, 96 widen, 66 are exponentials
+// and 128 rescale at need.  1.5 us a tile alone on a CU, 2.1 beside a group of few rows (512 rows over 32K tokens 108 us, 147 when
+// 32 rows at a time were streamed).  Its loop takes all 256 registers at D = 128: the compiler spills 13 to 36 in these kernels, most of
+// them at a piece's ends, one or two reads of them in the last slots of a step.
 // ---------------------------------------------------------------------------
 template <int D, int B>
 __device__ __forceinline__ void tile_piece(const Args& x, const Piece& p, char* smem) {

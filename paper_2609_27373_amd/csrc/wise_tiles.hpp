@@ -137,10 +137,11 @@ __device__ __forceinline__ int score_key(int t, int r, int h) {
 // more), or in fp16 beside a V in fp16 (11 bits).  fp16 has 15 binades above 1 and 14 below before it
 // loses bits: a row's reference m is then kept kHalfLow below its largest score and raised only when a score is
 // kHalfTop above it, so that what rounds to a subnormal weighs less than 2^-20 of the row's largest, and no
-// probability passes 2^14.  The sums of a row then lie up to 2^14 higher.  Both hold for references within
-// kHalfReach, where fp32 has steps of 2^-3 at most; at 2^29 a step is 64 and a probability may be 2^32 or 2^-32.
+// probability passes 2^14.  The sums of a row then lie up to 2^14 higher.  For that references have to be within
+// kHalfReach, where fp32 has steps of 2^-2 (and a probability may pass 2^14 by 2^0.75); at 2^29 a step is 64 and a probability
+// may be 2^32 or 2^-32.
 enum { kProbBf16, kProbSplit, kProbHalf };
-constexpr float kHalfLow = 6.f, kHalfTop = 14.f, kHalfReach = 0x1p20f;
+constexpr float kHalfLow = 6.f, kHalfTop = 14.f, kHalfReach = 0x1p22f;
 
 // ---------------------------------------------------------------------------
 // Per-wave state and steps of the tile engine.

@@ -1,4 +1,4 @@
-"""wise_qcache_attn on the GPU where numbers are very large: scores past 2^16 and up to fp32's largest, against the
+"""wise_qcache_attn on the GPU where numbers are very large: scores of 2^14 to fp32's largest, against the
 fp64 definition over scores that fp32 holds exactly, and values whose sums reach the end of its range."""
 
 import numpy as np
