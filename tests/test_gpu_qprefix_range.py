@@ -100,3 +100,41 @@ def test_large_values(gpu_lib, kind, d, gain, bits):
                 say(f"scale {which} d {d} bits {bits} {kind} gain {gain} shared {shared}")
                 assert torch.isfinite(out).all()
                 b.check(out, lse, truth)
+
+
+@WIDTHS
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("first", [False, True])
+def test_scores_that_overflow(gpu_lib, kind, d, first, bits):
+    """Keys of the largest values there are, whose scores are past fp32's range below or next to its end: they have weight 0, whether the
+    rows meet them first or last, and a row whose every score is -inf, like one that sees nothing, is 0."""
+    groups, kv, gq, q_len = KINDS[kind]
+    b = Batch(groups, 16, d, kv, gq, bits, q_len, seed=d)
+    big = {4: 6 * 2.0 ** 125, 8: 448 * 2.0 ** 119}[bits]
+    b.q[..., 0] = 1 + b.q[..., 0].abs()
+    b.q[0, :, :, 0] = 0.5                             # scores that stay finite
+    x = b.k.copy()
+    x[~np.isfinite(x)] = 0
+    x[..., 0] = np.abs(x[..., 0])
+    for s in b.ids:
+        at = 0 if first else int(b.lens[s] - 1) // 16
+        x[int(b.tables[s, at]), :, :, 0] = -big
+    codes, scales = quantise(x, bits)
+    pool = b.pool.copy()
+    pool[0] = pack(codes, scales, bits, 0)
+    b.set_pool(pool, 16, d, bits)
+    b.cache.pool.copy_(torch.tensor(pool))
+    near = b.k.copy()                                 # the definition, and bounds that know of no overflow, with scores of -80 and less
+    near[near == -big] = -2000
+    hold, b.k = b.k, near
+    o, _, bound, _ = b.truth()
+    b.k = hold
+    for cache in (b.cache, b.roomy()):
+        for shared in (True, False):
+            out, lse = b.run(shared, cache=cache)
+            say(f"d {d} bits {bits} {kind} first {first} shared {shared}")
+            got = out.double().cpu().numpy()
+            seen = np.isfinite(lse.cpu().numpy())     # a row may see those keys alone
+            assert np.isfinite(got).all() and np.all(got[~seen] == 0)
+            assert np.all(np.abs(got - o)[seen] <= bound[seen])
