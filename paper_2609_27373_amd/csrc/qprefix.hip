@@ -9,8 +9,8 @@
 // is exact too, which their scales tell (past_half), and meet probabilities of 11 bits in one MFMA: o is off by
 // 2^-12 of sum p |v| at most beside its own rounding of 2^-8, and measures 0.16 to 0.17% rms from its definition as
 // with exact probabilities.  Else, and where a row's reference is past kHalfReach, both are bf16 and a probability is two numbers
-// (split_bf16x2), an MFMA more.  One number instead of two everywhere took 32 x 8K tokens from 45 to 44 us, 128 over a 32K document from 203
-// to 171.
+// (split_bf16x2), an MFMA more.  Two everywhere would take 32 sequences of up to 8K tokens from 42 to 43 us, 128 over a 32K document from
+// 150 to 190 in 4 bits and from 183 to 277 in 8.
 #include "kept.hpp"
 #include "prefix_plan.hpp"
 
